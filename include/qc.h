@@ -56,6 +56,8 @@ typedef enum { QC_OUT_F32 = 0, QC_OUT_BF16 = 1, QC_OUT_I32_ACC = 2 } qc_out;
 #define QC_MAX_K 131072
 /* Largest number of output channels (the GEMM addresses a row of Y with 32-bit lane offsets). */
 #define QC_MAX_N 67108864
+/* Most experts of one grouped linear. */
+#define QC_MAX_EXPERTS 1024
 /* Most earlier tensors one qc_cumulative_variation call compares against. */
 #define QC_MAX_PREV 8
 
@@ -262,6 +264,60 @@ qc_status qc_qlinear_tensor(const void *X, qc_dtype xdt, int64_t M, int64_t K, i
                             const void *packed, const float *w_scale, int bits, int64_t N,
                             const float *bias, qc_epilogue epi, void *Y, qc_out ydt,
                             void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- 8-bit floating point with a scale for every block of 128 --------------------------------
+ * The linear on e4m3 operands (sign, 4 exponent and 3 fraction bits, largest number 448) that blockwise checkpoints
+ * are made of: a scale for every 128 consecutive columns of a token, computed online, and one for every 128 x 128 of
+ * the weights.  For a block with the largest magnitude a, every step one IEEE binary32 operation:
+ *      s = max(a, 2^-64) / 448
+ *      q = e4m3(x / s)                               to nearest, ties to even; a zero code may have either sign
+ *      Y[m, n] = act( sum_b s_x[m, b] s_w[n / 128, b] sum_{k in block b} q_x[m, k] q_w[n, k] + bias[n] )
+ * The last block of a row or column may be short; N and K are otherwise free.  With QC_OUT_F32 all sums are binary32 ones.
+ * With QC_OUT_BF16 the products of a block go through the matrix unit's e4m3 form, which keeps 13 bits below the largest of
+ * every eight products (1.5e-5 of a sum, by far less than the rounding to bf16); the blocks are added in binary32.  The order depends
+ * on the sizes of the call, so the same token may differ in the last bits between calls of other sizes, never between
+ * calls of the same.  A NaN or an infinity in X makes its token's outputs NaN and touches no other token's.
+ *   qc_pack_weight_fp8    W: device, float [experts, N, K] (experts = 1: one linear's matrix).  packed: device,
+ *                         qc_packed_weight_fp8_bytes(experts, N, K) bytes, 256-byte aligned, opaque.  w_scale:
+ *                         device, float [experts, ceil(N / 128), ceil(K / 128)]
+ *   qc_unpack_weight_codes_fp8   test hook: the codes of a packed blob, uint8 [experts, N, K]
+ *   qc_quant_act_fp8      qx: device, uint8 [M, K]; x_scale: device, float [M, ceil(K / 128)]
+ *   qc_qlinear_fp8        quantize + GEMM + epilogue.  workspace >= qc_qlinear_fp8_workspace_bytes(M, K, N) bytes,
+ *                         256-byte aligned, contents irrelevant on entry and unspecified on exit.  Y: QC_OUT_F32 or
+ *                         QC_OUT_BF16; may lie over X as for qc_qlinear
+ *   qc_qlinear_fp8_quant, qc_qlinear_fp8_gemm   two halves as calls of their own, for one input of several linears: the
+ *                         first leaves codes and scales in the workspace, the second may run on them repeatedly.  Their result
+ *                         and qc_qlinear_fp8's agree to the order of their sums
+ *   qc_qlinear_fp8_grouped   the linear of a mixture of experts.  The rows of X come sorted by expert:
+ *                         expert_offsets: device, int32 [experts + 1], read during the call's launches; rows
+ *                         expert_offsets[e] .. expert_offsets[e + 1] - 1 of X, and those of Y, are multiplied with expert e's
+ *                         weights and get its bias, bias [experts, N].  A group may be empty.  Rows before the first
+ *                         and behind the last group are not read as numbers and their rows of Y stay as they were.
+ *                         0 <= expert_offsets[e] <= expert_offsets[e + 1] <= M; of others the result is
+ *                         unspecified, but nothing outside X, Y and the workspace is touched.  Same
+ *                         workspace as qc_qlinear_fp8
+ * Errors as for qc_qlinear; UNSUPPORTED also: QC_OUT_I32_ACC, experts > QC_MAX_EXPERTS, M >= 2^31, and sizes for which a launch
+ * would need more than 2^24 blocks. */
+#define QC_FP8_BLOCK 128
+size_t qc_packed_weight_fp8_bytes(int64_t experts, int64_t N, int64_t K);
+qc_status qc_pack_weight_fp8(const float *W, int64_t experts, int64_t N, int64_t K, void *packed, float *w_scale,
+                             void *stream);
+qc_status qc_unpack_weight_codes_fp8(const void *packed, int64_t experts, int64_t N, int64_t K, uint8_t *codes,
+                                     void *stream);
+qc_status qc_quant_act_fp8(const void *X, qc_dtype xdt, int64_t M, int64_t K, uint8_t *qx, float *x_scale, void *stream);
+size_t qc_qlinear_fp8_workspace_bytes(int64_t M, int64_t K, int64_t N);
+qc_status qc_qlinear_fp8(const void *X, qc_dtype xdt, int64_t M, int64_t K, const void *packed, const float *w_scale,
+                         int64_t N, const float *bias, qc_epilogue epi, void *Y, qc_out ydt, void *workspace,
+                         size_t workspace_bytes, void *stream);
+qc_status qc_qlinear_fp8_quant(const void *X, qc_dtype xdt, int64_t M, int64_t K, void *workspace, size_t workspace_bytes,
+                               void *stream);
+qc_status qc_qlinear_fp8_gemm(const void *workspace, size_t workspace_bytes, int64_t M, int64_t K, const void *packed,
+                              const float *w_scale, int64_t N, const float *bias, qc_epilogue epi, void *Y, qc_out ydt,
+                              void *stream);
+qc_status qc_qlinear_fp8_grouped(const void *X, qc_dtype xdt, int64_t M, int64_t K, const int32_t *expert_offsets,
+                                 int64_t experts, const void *packed, const float *w_scale, int64_t N, const float *bias,
+                                 qc_epilogue epi, void *Y, qc_out ydt, void *workspace, size_t workspace_bytes,
+                                 void *stream);
 
 /* Test hook: after qc_qlinear(.., M, K, .., workspace, ..) returned QC_OK, copy the
  * activation codes and scales it used out of the workspace in canonical order:

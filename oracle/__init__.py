@@ -32,6 +32,7 @@ Paper passages each function follows (arxiv 2503.06545):
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import subprocess
 
@@ -404,3 +405,85 @@ def qlinear_tensor(X, qw, sw, bias=None, epi=EPI_NONE, act_bits: int = 8):
     acc = gemm_i32(qx, qw)
     y = epilogue(acc, np.full(X.shape[0], s, np.float32), sw, bias, epi)
     return {"qx": qx, "sx": s, "acc": acc, "y": y}
+
+
+# ---- 8-bit floating point with a scale for every block of 128 -----------------------------------
+# e4m3: 1.fff * 2^e with e from -6 to 8, below that steps of 2^-9, largest 448 (the pattern above it is a NaN).
+
+FP8_BLOCK = 128
+FP8_MOST = 448.0
+
+
+def _e4m3_table():
+    """The value of each of the 256 patterns."""
+    code = np.arange(256)
+    e, f = (code >> 3) & 15, code & 7
+    v = np.where(e == 0, f * 2.0 ** -9, (8 + f) * 2.0 ** (e - 10.0))
+    v[(code & 127) == 127] = np.nan
+    return np.where(code & 128, -v, v)
+
+
+E4M3 = _e4m3_table()
+
+
+def e4m3_values(codes):
+    return E4M3[np.asarray(codes, np.uint8)]
+
+
+def e4m3_codes(x):
+    """Nearest codes of finite values of magnitude 448 at most, ties to the even code; a zero keeps its sign."""
+    x = np.asarray(x, np.float64)
+    a, table = np.abs(x), E4M3[:127]
+    hi = np.minimum(np.searchsorted(table, a), 126)   # the first code at or above
+    lo = np.maximum(hi - 1, 0)
+    up, down = table[hi] - a, a - table[lo]           # exact: few bits apart
+    code = np.where((down < up) | ((down == up) & (lo % 2 == 0)), lo, hi).astype(np.uint8)
+    return code | (np.signbit(x).astype(np.uint8) << 7)
+
+
+def _blocks(a, axis):
+    """The largest magnitude of each run of 128 along an axis, and the index of its run for every element."""
+    n = a.shape[axis]
+    starts = np.arange(0, n, FP8_BLOCK)
+    return np.maximum.reduceat(np.abs(a), starts, axis=axis), np.arange(n) // FP8_BLOCK
+
+
+def _fp8_scale(largest):
+    return np.maximum(largest.astype(np.float32), np.float32(2.0 ** -64)) / np.float32(FP8_MOST)
+
+
+def quant_act_fp8(X):
+    """(uint8 codes [M, K], float32 scales [M, ceil(K / 128)]) of rows, one scale for every 128 columns."""
+    x = widen_f32(X)
+    largest, block = _blocks(x, 1)
+    s = _fp8_scale(largest)
+    return e4m3_codes(x / s[:, block]), s
+
+
+def quant_weight_fp8(W):
+    """(uint8 codes [N, K], float32 scales [ceil(N / 128), ceil(K / 128)])."""
+    W = _c(W, np.float32)
+    rows, nb = _blocks(W, 0)
+    largest, kb = _blocks(rows, 1)
+    s = _fp8_scale(largest)
+    return e4m3_codes(W / s[nb][:, kb]), s
+
+
+def qlinear_fp8(X, qw, sw, bias=None, epi=EPI_NONE):
+    """The linear in 64 bits: dict(y, size), size the sum of the magnitudes that went into each output before the
+    activation, which bounds what rounding can do to it."""
+    qx, sx = quant_act_fp8(X)
+    kb = np.arange(qx.shape[1]) // FP8_BLOCK
+    x = e4m3_values(qx) * sx.astype(np.float64)[:, kb]
+    w = e4m3_values(qw) * sw.astype(np.float64)[np.arange(len(qw)) // FP8_BLOCK][:, kb]
+    b = np.zeros(len(qw)) if bias is None else np.asarray(bias, np.float64)
+    y, size = x @ w.T + b, np.abs(x) @ np.abs(w).T + np.abs(b)
+    if epi != EPI_NONE:
+        y = np.array([_gelu(v, epi) for v in y.reshape(-1)]).reshape(y.shape)
+    return {"qx": qx, "sx": sx, "y": y, "size": size}
+
+
+def _gelu(v, epi):
+    if epi == EPI_GELU_TANH:
+        return 0.5 * v * (1.0 + math.tanh(math.sqrt(2.0 / math.pi) * (v + 0.044715 * v ** 3)))
+    return 0.5 * v * math.erfc(-v / math.sqrt(2.0))

@@ -21,6 +21,8 @@ QC_OUT_F32, QC_OUT_BF16, QC_OUT_I32_ACC = 0, 1, 2
 QC_MAX_K = 131072
 QC_MAX_N = 67108864
 QC_MAX_PREV = 8
+QC_MAX_EXPERTS = 1024
+QC_FP8_BLOCK = 128
 
 EXPORTS = (
     "qc_status_string", "qc_version", "qc_packed_weight_bytes", "qc_qlinear_workspace_bytes",
@@ -38,6 +40,9 @@ EXPORTS = (
     "qc_qlinear_asym", "qc_debug_workspace_act_asym", "qc_qlinear_asym_quant",
     "qc_qlinear_asym_gemm", "qc_quant_act_tensor_workspace_bytes", "qc_quant_act_tensor",
     "qc_qlinear_tensor_workspace_bytes", "qc_qlinear_tensor", "qc_latent_delta_static",
+    "qc_packed_weight_fp8_bytes", "qc_pack_weight_fp8", "qc_unpack_weight_codes_fp8", "qc_quant_act_fp8",
+    "qc_qlinear_fp8_workspace_bytes", "qc_qlinear_fp8", "qc_qlinear_fp8_quant", "qc_qlinear_fp8_gemm",
+    "qc_qlinear_fp8_grouped",
 )
 
 
@@ -145,6 +150,24 @@ def lib() -> ctypes.CDLL:
         L.qc_cumulative_variation_workspace_bytes.argtypes = [i64, i32]
         L.qc_cumulative_variation.restype = i32
         L.qc_cumulative_variation.argtypes = [vp, ctypes.POINTER(vp), i32, i64, vp, vp, sz, vp]
+        L.qc_packed_weight_fp8_bytes.restype = sz
+        L.qc_packed_weight_fp8_bytes.argtypes = [i64, i64, i64]
+        L.qc_pack_weight_fp8.restype = i32
+        L.qc_pack_weight_fp8.argtypes = [vp, i64, i64, i64, vp, vp, vp]
+        L.qc_unpack_weight_codes_fp8.restype = i32
+        L.qc_unpack_weight_codes_fp8.argtypes = [vp, i64, i64, i64, vp, vp]
+        L.qc_quant_act_fp8.restype = i32
+        L.qc_quant_act_fp8.argtypes = [vp, i32, i64, i64, vp, vp, vp]
+        L.qc_qlinear_fp8_workspace_bytes.restype = sz
+        L.qc_qlinear_fp8_workspace_bytes.argtypes = [i64, i64, i64]
+        L.qc_qlinear_fp8.restype = i32
+        L.qc_qlinear_fp8.argtypes = [vp, i32, i64, i64, vp, vp, i64, vp, i32, vp, i32, vp, sz, vp]
+        L.qc_qlinear_fp8_quant.restype = i32
+        L.qc_qlinear_fp8_quant.argtypes = [vp, i32, i64, i64, vp, sz, vp]
+        L.qc_qlinear_fp8_gemm.restype = i32
+        L.qc_qlinear_fp8_gemm.argtypes = [vp, sz, i64, i64, vp, vp, i64, vp, i32, vp, i32, vp]
+        L.qc_qlinear_fp8_grouped.restype = i32
+        L.qc_qlinear_fp8_grouped.argtypes = [vp, i32, i64, i64, vp, i64, vp, vp, i64, vp, i32, vp, i32, vp, sz, vp]
         L.qc_divergence_score.restype = f32
         L.qc_divergence_score.argtypes = [f32, i32, f32]
         L.qc_cache_interval.restype = i32
@@ -353,6 +376,45 @@ def qc_qlinear_tensor(X, xdt, M, K, act_bits, packed, w_scale, bits, N, bias, ep
 def qc_debug_workspace_act_asym(workspace, M, K, act_bits, qx, x_scale, x_zero, stream=0) -> int:
     return int(lib().qc_debug_workspace_act_asym(workspace, M, K, act_bits, qx, x_scale, x_zero,
                                                  stream))
+
+
+def qc_packed_weight_fp8_bytes(experts: int, N: int, K: int) -> int:
+    return int(lib().qc_packed_weight_fp8_bytes(experts, N, K))
+
+
+def qc_pack_weight_fp8(W, experts, N, K, packed, w_scale, stream=0) -> int:
+    return int(lib().qc_pack_weight_fp8(W, experts, N, K, packed, w_scale, stream))
+
+
+def qc_unpack_weight_codes_fp8(packed, experts, N, K, codes, stream=0) -> int:
+    return int(lib().qc_unpack_weight_codes_fp8(packed, experts, N, K, codes, stream))
+
+
+def qc_quant_act_fp8(X, xdt, M, K, qx, x_scale, stream=0) -> int:
+    return int(lib().qc_quant_act_fp8(X, xdt, M, K, qx, x_scale, stream))
+
+
+def qc_qlinear_fp8_workspace_bytes(M: int, K: int, N: int) -> int:
+    return int(lib().qc_qlinear_fp8_workspace_bytes(M, K, N))
+
+
+def qc_qlinear_fp8(X, xdt, M, K, packed, w_scale, N, bias, epi, Y, ydt, workspace, workspace_bytes, stream=0) -> int:
+    return int(lib().qc_qlinear_fp8(X, xdt, M, K, packed, w_scale, N, bias, epi, Y, ydt, workspace, workspace_bytes,
+                                    stream))
+
+
+def qc_qlinear_fp8_quant(X, xdt, M, K, workspace, workspace_bytes, stream=0) -> int:
+    return int(lib().qc_qlinear_fp8_quant(X, xdt, M, K, workspace, workspace_bytes, stream))
+
+
+def qc_qlinear_fp8_gemm(workspace, workspace_bytes, M, K, packed, w_scale, N, bias, epi, Y, ydt, stream=0) -> int:
+    return int(lib().qc_qlinear_fp8_gemm(workspace, workspace_bytes, M, K, packed, w_scale, N, bias, epi, Y, ydt, stream))
+
+
+def qc_qlinear_fp8_grouped(X, xdt, M, K, expert_offsets, experts, packed, w_scale, N, bias, epi, Y, ydt, workspace,
+                           workspace_bytes, stream=0) -> int:
+    return int(lib().qc_qlinear_fp8_grouped(X, xdt, M, K, expert_offsets, experts, packed, w_scale, N, bias, epi, Y, ydt,
+                                            workspace, workspace_bytes, stream))
 
 
 def qc_frame_gradient_norm_workspace_bytes(frames: int, inner: int) -> int:
@@ -691,6 +753,124 @@ def qlinear_tensor_t(X, pw: PackedWeight, bias=None, epi="none", out="bf16", wor
                              None if bias is None else bias.data_ptr(), EPI[epi], Y.data_ptr(),
                              OUT[out], workspace.data_ptr(), workspace.numel(), _stream()),
            "qc_qlinear_tensor")
+    return Y
+
+
+# ---- 8-bit floating point with a scale for every block of 128 -------------------------------------
+
+class PackedWeightFp8:
+    """Device blob written by qc_pack_weight_fp8 plus its scales, float [experts, ceil(N / 128), ceil(K / 128)]."""
+
+    def __init__(self, blob, scale, experts: int, N: int, K: int):
+        self.blob, self.scale, self.experts, self.N, self.K = blob, scale, experts, N, K
+
+
+def _fp8_operand(t, name, dtypes, shape, device=None) -> None:
+    """A dense tensor of this shape (None: any length) on the current device, which the launch goes to."""
+    torch = _torch()
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    if t.dim() != len(shape) or any(want is not None and got != want for got, want in zip(t.shape, shape)):
+        raise ValueError(f"{name} must be {['any' if n is None else n for n in shape]}, got {list(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current GPU, got {t.device}")
+
+
+def _fp8_activation(X, K=None) -> None:
+    torch = _torch()
+    _fp8_operand(X, "X", (torch.float32, torch.bfloat16), (None, K))
+
+
+def pack_weight_fp8_t(W) -> PackedWeightFp8:
+    """W float32 [N, K], or [experts, N, K] for the grouped linear."""
+    torch = _torch()
+    _fp8_operand(W, "W", (torch.float32,), (None,) * (3 if W.dim() == 3 else 2))
+    E, (N, K) = W.shape[0] if W.dim() == 3 else 1, W.shape[-2:]
+    nbytes = qc_packed_weight_fp8_bytes(E, N, K)
+    if nbytes == 0:
+        raise QcError(QC_ERR_UNSUPPORTED, "qc_packed_weight_fp8_bytes")
+    blob = torch.empty(nbytes, dtype=torch.uint8, device=W.device)
+    scale = torch.empty((E, -(-N // QC_FP8_BLOCK), -(-K // QC_FP8_BLOCK)), dtype=torch.float32, device=W.device)
+    _check(qc_pack_weight_fp8(W.data_ptr(), E, N, K, blob.data_ptr(), scale.data_ptr(), _stream()), "qc_pack_weight_fp8")
+    return PackedWeightFp8(blob, scale, E, N, K)
+
+
+def unpack_weight_codes_fp8_t(pw: PackedWeightFp8):
+    """The codes, float8_e4m3fn [experts, N, K]."""
+    torch = _torch()
+    codes = torch.empty((pw.experts, pw.N, pw.K), dtype=torch.uint8, device=pw.blob.device)
+    _check(qc_unpack_weight_codes_fp8(pw.blob.data_ptr(), pw.experts, pw.N, pw.K, codes.data_ptr(), _stream()),
+           "qc_unpack_weight_codes_fp8")
+    return codes.view(torch.float8_e4m3fn)
+
+
+def quant_act_fp8_t(X, qx=None, x_scale=None):
+    """X [M, K] -> codes float8_e4m3fn [M, K], scales float32 [M, ceil(K / 128)]; into qx and x_scale if given."""
+    torch = _torch()
+    _fp8_activation(X)
+    M, K = X.shape
+    if qx is None:
+        qx = torch.empty((M, K), dtype=torch.float8_e4m3fn, device=X.device)
+    else:
+        _fp8_operand(qx, "qx", (torch.float8_e4m3fn,), (M, K))
+    if x_scale is None:
+        x_scale = torch.empty((M, -(-K // QC_FP8_BLOCK)), dtype=torch.float32, device=X.device)
+    else:
+        _fp8_operand(x_scale, "x_scale", (torch.float32,), (M, -(-K // QC_FP8_BLOCK)))
+    _check(lib().qc_quant_act_fp8(X.data_ptr(), _xdt(X), M, K, qx.data_ptr(), x_scale.data_ptr(), _stream()),
+           "qc_quant_act_fp8")
+    return qx, x_scale
+
+
+def qlinear_fp8_workspace_t(M: int, K: int, N: int, device="cuda"):
+    """For qlinear_fp8_t and qlinear_fp8_grouped_t on M rows."""
+    torch = _torch()
+    nbytes = qc_qlinear_fp8_workspace_bytes(M, K, N)
+    if nbytes == 0:
+        raise QcError(QC_ERR_UNSUPPORTED, "qc_qlinear_fp8_workspace_bytes")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _fp8_linear_operands(X, pw, bias, out, workspace, Y, bias_shape):
+    torch = _torch()
+    _fp8_activation(X, pw.K)
+    ydtype = {"f32": torch.float32, "bf16": torch.bfloat16}[out]
+    if bias is not None:
+        _fp8_operand(bias, "bias", (torch.float32,), bias_shape)
+    if workspace is None:
+        workspace = qlinear_fp8_workspace_t(X.shape[0], pw.K, pw.N, X.device)
+    else:
+        _fp8_operand(workspace, "workspace", (torch.uint8,), (None,))
+    if Y is None:
+        Y = torch.empty((X.shape[0], pw.N), dtype=ydtype, device=X.device)
+    else:
+        _fp8_operand(Y, "Y", (ydtype,), (X.shape[0], pw.N))
+    return workspace, Y
+
+
+def qlinear_fp8_t(X, pw: PackedWeightFp8, bias=None, epi="none", out="bf16", workspace=None, Y=None):
+    """X [M, K] float32 or bfloat16, pw of one matrix, bias float32 [N] -> Y [M, N]."""
+    if pw.experts != 1:
+        raise ValueError(f"a linear has one weight matrix, pw holds {pw.experts}: qlinear_fp8_grouped_t")
+    workspace, Y = _fp8_linear_operands(X, pw, bias, out, workspace, Y, (pw.N,))
+    _check(lib().qc_qlinear_fp8(X.data_ptr(), _xdt(X), X.shape[0], pw.K, pw.blob.data_ptr(), pw.scale.data_ptr(), pw.N,
+                                None if bias is None else bias.data_ptr(), EPI[epi], Y.data_ptr(), OUT[out],
+                                workspace.data_ptr(), workspace.numel(), _stream()), "qc_qlinear_fp8")
+    return Y
+
+
+def qlinear_fp8_grouped_t(X, pw: PackedWeightFp8, expert_offsets, bias=None, epi="none", out="bf16", workspace=None, Y=None):
+    """X [M, K], its rows sorted by expert; expert_offsets int32 [experts + 1] on the GPU; bias float32 [experts, N]
+    -> Y [M, N], in which rows of no group stay as they were."""
+    torch = _torch()
+    _fp8_operand(expert_offsets, "expert_offsets", (torch.int32,), (pw.experts + 1,))
+    workspace, Y = _fp8_linear_operands(X, pw, bias, out, workspace, Y, (pw.experts, pw.N))
+    _check(lib().qc_qlinear_fp8_grouped(X.data_ptr(), _xdt(X), X.shape[0], pw.K, expert_offsets.data_ptr(), pw.experts,
+                                        pw.blob.data_ptr(), pw.scale.data_ptr(), pw.N,
+                                        None if bias is None else bias.data_ptr(), EPI[epi], Y.data_ptr(), OUT[out],
+                                        workspace.data_ptr(), workspace.numel(), _stream()), "qc_qlinear_fp8_grouped")
     return Y
 
 

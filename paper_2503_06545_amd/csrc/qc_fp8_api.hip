@@ -1,0 +1,161 @@
+// C ABI entry points of the 8-bit floating-point linear: argument checks first, then launches on the caller's
+// stream.  Nothing here allocates or synchronises.
+#include "qc_fp8.h"
+
+using namespace qc;
+
+namespace {
+
+bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+constexpr int64_t kBlocksMost = 0xffffffffLL / 256;   // of 256 threads in a launch
+
+#define QC_TRY(expr)                          \
+    do {                                      \
+        const qc_status st_ = (expr);         \
+        if (st_ != QC_OK) return st_;         \
+    } while (0)
+
+qc_status device_status(hipError_t e) { return e == hipSuccess ? QC_OK : QC_ERR_DEVICE; }
+
+// INVALID_ARG (pointers, sizes, enums, alignment), then UNSUPPORTED, then WORKSPACE, as for the integer linears
+
+qc_status check_activation(const void *X, qc_dtype xdt, int64_t M, int64_t K) {
+    if (!X || M < 1 || K < 1) return QC_ERR_INVALID_ARG;
+    if (xdt != QC_F32 && xdt != QC_BF16) return QC_ERR_INVALID_ARG;
+    return aligned(X, 16) ? QC_OK : QC_ERR_INVALID_ARG;
+}
+
+qc_status check_weight_side(const void *packed, const float *w_scale, const float *bias, qc_epilogue epi, const void *Y,
+                            qc_out ydt, int64_t M, int64_t K, int64_t N) {
+    if (!packed || !w_scale || !Y || M < 1 || K < 1 || N < 1) return QC_ERR_INVALID_ARG;
+    if (epi != QC_EPI_NONE && epi != QC_EPI_GELU_TANH && epi != QC_EPI_GELU_ERF) return QC_ERR_INVALID_ARG;
+    if (ydt != QC_OUT_F32 && ydt != QC_OUT_BF16 && ydt != QC_OUT_I32_ACC) return QC_ERR_INVALID_ARG;
+    if (!aligned(packed, 256) || !aligned(w_scale, 16) || !aligned(Y, 16) || (bias && !aligned(bias, 16))) return QC_ERR_INVALID_ARG;
+    return QC_OK;
+}
+
+qc_status check_quant_supported(int64_t M, int64_t K) {
+    return K > QC_MAX_K || M > 0x7fffffffLL || (M + 31) / 32 * fp8_blocks(K) >= kBlocksMost ? QC_ERR_UNSUPPORTED : QC_OK;
+}
+
+qc_status check_gemm_supported(int64_t M, int64_t K, int64_t N, int64_t experts, qc_out ydt) {
+    if (ydt == QC_OUT_I32_ACC || M > 0x7fffffffLL || qc_packed_weight_fp8_bytes(experts, N, K) == 0) return QC_ERR_UNSUPPORTED;
+    const int64_t tiles = M / kFp8TokensLeast + experts;
+    return tiles * (round_up(N, kTileN) / kTileN) > kBlocksMost ? QC_ERR_UNSUPPORTED : QC_OK;
+}
+
+qc_status check_workspace(const void *workspace) { return workspace && aligned(workspace, 256) ? QC_OK : QC_ERR_INVALID_ARG; }
+
+qc_status gemm(const void *workspace, int64_t M, int64_t K, const void *packed, const float *w_scale, int64_t N, const float *bias,
+               qc_epilogue epi, void *Y, qc_out ydt, int experts, int tokens, bool grouped, void *stream) {
+    const Fp8Workspace ws = fp8_workspace(M, K);
+    const uint8_t *const base = (const uint8_t *)workspace;
+    Fp8GemmArgs a{};
+    a.x_tiled = base + ws.codes_offset;
+    a.x_scale = (const float *)base;
+    a.w_codes = (const uint8_t *)packed + kPackedHeaderBytes;
+    a.w_scale = w_scale;
+    a.bias = bias;
+    a.Y = Y;
+    a.map = grouped ? (const Fp8Tile *)(base + ws.map_offset) : nullptr;
+    a.M = M;
+    a.N = N;
+    a.Mp = ws.Mp;
+    a.w_expert_bytes = fp8_weight_bytes(N, K);
+    a.KB = (int)ws.KB;
+    a.m_tiles = (int)(grouped ? fp8_tiles_most(M, experts, tokens) : (M + tokens - 1) / tokens);
+    a.n_tiles = (int)(round_up(N, kTileN) / kTileN);
+    return device_status(launch_fp8_gemm(a, tokens, epi, ydt, (hipStream_t)stream));
+}
+
+}  // namespace
+
+extern "C" size_t qc_packed_weight_fp8_bytes(int64_t experts, int64_t N, int64_t K) {
+    if (experts < 1 || N < 1 || K < 1 || experts > QC_MAX_EXPERTS || N > QC_MAX_N || K > QC_MAX_K) return 0;
+    if (experts * (round_up(N, kTileN) / kTileN) * fp8_blocks(K) > kBlocksMost) return 0;
+    return (size_t)kPackedHeaderBytes + (size_t)experts * (size_t)fp8_weight_bytes(N, K);
+}
+
+extern "C" qc_status qc_pack_weight_fp8(const float *W, int64_t experts, int64_t N, int64_t K, void *packed, float *w_scale,
+                                        void *stream) {
+    if (!W || !packed || !w_scale || experts < 1 || N < 1 || K < 1) return QC_ERR_INVALID_ARG;
+    if (!aligned(W, 16) || !aligned(packed, 256) || !aligned(w_scale, 16)) return QC_ERR_INVALID_ARG;
+    if (qc_packed_weight_fp8_bytes(experts, N, K) == 0) return QC_ERR_UNSUPPORTED;
+    return device_status(launch_fp8_pack(W, experts, N, K, (uint8_t *)packed, w_scale, (hipStream_t)stream));
+}
+
+extern "C" qc_status qc_unpack_weight_codes_fp8(const void *packed, int64_t experts, int64_t N, int64_t K, uint8_t *codes,
+                                                void *stream) {
+    if (!packed || !codes || experts < 1 || N < 1 || K < 1 || !aligned(packed, 256)) return QC_ERR_INVALID_ARG;
+    if (qc_packed_weight_fp8_bytes(experts, N, K) == 0) return QC_ERR_UNSUPPORTED;
+    return device_status(launch_fp8_unpack((const uint8_t *)packed, experts, N, K, codes, (hipStream_t)stream));
+}
+
+extern "C" qc_status qc_quant_act_fp8(const void *X, qc_dtype xdt, int64_t M, int64_t K, uint8_t *qx, float *x_scale, void *stream) {
+    QC_TRY(check_activation(X, xdt, M, K));
+    if (!qx || !x_scale || !aligned(qx, 16) || !aligned(x_scale, 4)) return QC_ERR_INVALID_ARG;
+    QC_TRY(check_quant_supported(M, K));
+    return device_status(launch_fp8_quant(X, xdt, M, K, qx, nullptr, x_scale, nullptr, 0, 0, nullptr, (hipStream_t)stream));
+}
+
+extern "C" size_t qc_qlinear_fp8_workspace_bytes(int64_t M, int64_t K, int64_t N) {
+    if (M < 1 || K < 1 || N < 1 || K > QC_MAX_K) return 0;
+    return fp8_workspace(M, K).total_bytes;
+}
+
+extern "C" qc_status qc_qlinear_fp8_quant(const void *X, qc_dtype xdt, int64_t M, int64_t K, void *workspace, size_t workspace_bytes,
+                                          void *stream) {
+    QC_TRY(check_activation(X, xdt, M, K));
+    QC_TRY(check_workspace(workspace));
+    QC_TRY(check_quant_supported(M, K));
+    const Fp8Workspace ws = fp8_workspace(M, K);
+    if (workspace_bytes < ws.total_bytes) return QC_ERR_WORKSPACE;
+    uint8_t *const base = (uint8_t *)workspace;
+    return device_status(launch_fp8_quant(X, xdt, M, K, nullptr, base + ws.codes_offset, (float *)base, nullptr, 0, 0, nullptr,
+                                          (hipStream_t)stream));
+}
+
+extern "C" qc_status qc_qlinear_fp8_gemm(const void *workspace, size_t workspace_bytes, int64_t M, int64_t K, const void *packed,
+                                         const float *w_scale, int64_t N, const float *bias, qc_epilogue epi, void *Y, qc_out ydt,
+                                         void *stream) {
+    QC_TRY(check_weight_side(packed, w_scale, bias, epi, Y, ydt, M, K, N));
+    QC_TRY(check_workspace(workspace));
+    QC_TRY(check_gemm_supported(M, K, N, 1, ydt));
+    if (workspace_bytes < fp8_workspace(M, K).total_bytes) return QC_ERR_WORKSPACE;
+    return gemm(workspace, M, K, packed, w_scale, N, bias, epi, Y, ydt, 1, fp8_gemm_tokens(M, N, K, 1), false, stream);
+}
+
+extern "C" qc_status qc_qlinear_fp8(const void *X, qc_dtype xdt, int64_t M, int64_t K, const void *packed, const float *w_scale,
+                                    int64_t N, const float *bias, qc_epilogue epi, void *Y, qc_out ydt, void *workspace,
+                                    size_t workspace_bytes, void *stream) {
+    // both halves' checks up front, so that a failed call has no side effect
+    QC_TRY(check_activation(X, xdt, M, K));
+    QC_TRY(check_weight_side(packed, w_scale, bias, epi, Y, ydt, M, K, N));
+    QC_TRY(check_workspace(workspace));
+    QC_TRY(check_quant_supported(M, K));
+    QC_TRY(check_gemm_supported(M, K, N, 1, ydt));
+    if (workspace_bytes < fp8_workspace(M, K).total_bytes) return QC_ERR_WORKSPACE;
+    QC_TRY(qc_qlinear_fp8_quant(X, xdt, M, K, workspace, workspace_bytes, stream));
+    return qc_qlinear_fp8_gemm(workspace, workspace_bytes, M, K, packed, w_scale, N, bias, epi, Y, ydt, stream);
+}
+
+extern "C" qc_status qc_qlinear_fp8_grouped(const void *X, qc_dtype xdt, int64_t M, int64_t K, const int32_t *expert_offsets,
+                                            int64_t experts, const void *packed, const float *w_scale, int64_t N, const float *bias,
+                                            qc_epilogue epi, void *Y, qc_out ydt, void *workspace, size_t workspace_bytes,
+                                            void *stream) {
+    QC_TRY(check_activation(X, xdt, M, K));
+    QC_TRY(check_weight_side(packed, w_scale, bias, epi, Y, ydt, M, K, N));
+    if (!expert_offsets || !aligned(expert_offsets, 4) || experts < 1) return QC_ERR_INVALID_ARG;
+    QC_TRY(check_workspace(workspace));
+    if (experts > QC_MAX_EXPERTS) return QC_ERR_UNSUPPORTED;
+    QC_TRY(check_quant_supported(M, K));
+    QC_TRY(check_gemm_supported(M, K, N, experts, ydt));
+    const Fp8Workspace ws = fp8_workspace(M, K);
+    if (workspace_bytes < ws.total_bytes) return QC_ERR_WORKSPACE;
+    uint8_t *const base = (uint8_t *)workspace;
+    const int tokens = fp8_gemm_tokens(M, N, K, (int)experts);
+    QC_TRY(device_status(launch_fp8_quant(X, xdt, M, K, nullptr, base + ws.codes_offset, (float *)base, expert_offsets, (int)experts,
+                                          tokens, (Fp8Tile *)(base + ws.map_offset), (hipStream_t)stream)));
+    return gemm(workspace, M, K, packed, w_scale, N, bias, epi, Y, ydt, (int)experts, tokens, true, stream);
+}

@@ -1,0 +1,266 @@
+// Quantizers of the 8-bit floating-point linear: e4m3 codes, one scale for every 128 columns of a token (activations,
+// online) or every 128 x 128 (weights, offline).
+//
+//   s = max(max |x|, 2^-64) / 448,   q = e4m3(x / s)      both divisions IEEE binary32, the cast to nearest even
+//
+// HBM-bound: every element of X is read once and one code written.  A block of 128 columns is what eight lanes hold of a
+// row (see Group in qc_device.h), so a block's maximum is three DPP steps away and nothing has to wait for the rest of the
+// row.  The quotient is computed as in qc_quant.hip, from one division per block; values whose quotient is too small for
+// that to be exact round to a zero code either way.
+#include "qc_device.h"
+#include "qc_fp8.h"
+
+namespace qc {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kRowsPerWave = 8;   // eight lanes each
+
+// eight lanes' share of columns col0 .. col0 + 127 of a row of K at any alignment, zeros past its end
+template <typename XT, bool NT>
+__device__ inline void load_block(Group<XT> &g, const XT *xrow, int64_t col0, int64_t K, int sub) {
+    constexpr int E = 16 / (int)sizeof(XT), P = sizeof(g.v) / sizeof(g.v[0]);
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+        const int64_t col = col0 + 8 * E * j + E * sub;
+        const int64_t past = col + E - K;   // elements of the piece past the row's end
+        if (past <= 0) {
+            const u32x4_any t = *reinterpret_cast<const u32x4_any *>(xrow + col);
+            g.v[j] = make_uint4(t.x, t.y, t.z, t.w);
+        } else if (past >= E) {
+            g.v[j] = make_uint4(0, 0, 0, 0);
+        } else if (K >= E) {   // loaded so that it ends with the row, and moved down
+            const u32x4_any t = *reinterpret_cast<const u32x4_any *>(xrow + K - E);
+            g.v[j] = move_down(make_uint4(t.x, t.y, t.z, t.w), (int)past * (int)(sizeof(XT) / 2));
+        } else {               // a row of less than 16 B
+            uint32_t w[4] = {0, 0, 0, 0};
+            for (int e = 0; e < (int)(E - past); ++e) {
+                if constexpr (sizeof(XT) == 4) w[e] = __float_as_uint(xrow[col + e]);
+                else w[e / 2] |= (uint32_t)xrow[col + e] << (16 * (e % 2));
+            }
+            g.v[j] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+
+// four quotients -> four e4m3 codes in a dword, element 0 lowest
+__device__ inline uint32_t e4m3x4(float q0, float q1, float q2, float q3) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(q0, q1, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q2, q3, w, true);
+}
+
+struct QuantArgs {
+    const void *X;
+    uint8_t *qx, *qx_tiled;
+    float *x_scale;
+    int64_t M, K, Mp;
+    int KB, chunks;
+    const int32_t *offsets;   // grouped only
+    Fp8Tile *map;
+    int experts, tokens, map_entries, quant_blocks;
+};
+
+// ---- the map of a grouped GEMM's tiles ----------------------------------------------------------
+// One block beside those that quantize.  A group is [lo_e, hi_e) with lo_e the largest of offsets 0 .. e and hi_e that of 0 .. e + 1, all
+// within 0 .. M: the groups of offsets in order, and for any others still disjoint rows inside the buffer, so that their
+// tiles never outnumber fp8_tiles_most().
+__device__ void make_map(const QuantArgs &a) {
+    __shared__ int32_t lo[QC_MAX_EXPERTS + 1], first[QC_MAX_EXPERTS + 1];
+    const int E = a.experts, M = (int)a.M;
+    if (threadIdx.x < 64) {   // one wavefront scans, each lane a run of experts
+        const int lane = threadIdx.x, per = (E + 64) / 64;   // E + 1 offsets
+        const int e0 = lane * per, e1 = min(e0 + per, E + 1);
+        int most = 0;
+        for (int e = e0; e < e1; ++e) most = max(most, min(a.offsets[e], M));
+        int before = most;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int v = __shfl_up(before, d);
+            if (lane >= d) before = max(before, v);
+        }
+        before = __shfl_up(before, 1);
+        if (lane == 0) before = 0;
+        for (int e = e0; e < e1; ++e) lo[e] = before = max(before, min(a.offsets[e], M));
+    }
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const int lane = threadIdx.x, per = (E + 63) / 64;
+        const int e0 = lane * per, e1 = min(e0 + per, E);
+        int tiles = 0;
+        for (int e = e0; e < e1; ++e) tiles += (lo[e + 1] - lo[e] + a.tokens - 1) / a.tokens;
+        int upto = tiles;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int v = __shfl_up(upto, d);
+            if (lane >= d) upto += v;
+        }
+        int at = upto - tiles;
+        for (int e = e0; e < e1; ++e) {
+            first[e] = at;
+            at += (lo[e + 1] - lo[e] + a.tokens - 1) / a.tokens;
+        }
+        if (lane == 63) first[E] = upto;
+    }
+    __syncthreads();
+    const int total = first[E];
+    for (int v = threadIdx.x; v < a.map_entries; v += kThreads) {
+        Fp8Tile t{0, 0, -1, 0};
+        if (v < total) {
+            int e = 0, end = E;   // the last expert that begins at or before v: the one with rows
+            while (end - e > 1) {
+                const int mid = (e + end) / 2;
+                if (first[mid] <= v) e = mid;
+                else end = mid;
+            }
+            t.expert = e;
+            t.row0 = lo[e] + (v - first[e]) * a.tokens;
+            t.rows = min(a.tokens, lo[e + 1] - t.row0);
+        }
+        a.map[v] = t;
+    }
+}
+
+// A wavefront takes eight rows x GROUPS blocks of 128 columns.
+template <typename XT, int GROUPS>
+__global__ __launch_bounds__(kThreads) void fp8_quant_kernel(QuantArgs a) {
+    if (a.map && (int)blockIdx.x == a.quant_blocks) {
+        make_map(a);
+        return;
+    }
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int sub = lane & 7;
+    const int64_t row_block = blockIdx.x / (uint32_t)a.chunks;
+    const int chunk = blockIdx.x % (uint32_t)a.chunks;
+    const int64_t row0 = (row_block * kWaves + wave) * kRowsPerWave, row = row0 + lane / 8;
+    if (row >= a.M) return;
+    if (a.map && (row < a.offsets[0] || row >= a.offsets[a.experts])) return;   // of no group
+    const XT *const xrow = reinterpret_cast<const XT *>(a.X) + row * a.K;
+    const int b0 = chunk * GROUPS;
+
+    Group<XT> g[GROUPS];
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) load_block<XT, false>(g[i], xrow, (int64_t)(b0 + i) * kFp8Block, a.K, sub);
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+        if (b0 + i >= a.KB) break;
+        auto running = Group<XT>::no_max();
+        g[i].absmax_into(running);
+        const float s = scale_of(max_of_eight(Group<XT>::absmax_value(running)), kE4m3Most);
+        const float r = 1.0f / s;
+        uint32_t w[4];
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+            w[d] = e4m3x4(quotient(g[i].get(4 * d + 0), s, r), quotient(g[i].get(4 * d + 1), s, r),
+                          quotient(g[i].get(4 * d + 2), s, r), quotient(g[i].get(4 * d + 3), s, r));
+        const uint4 out = Group<XT>::gather_codes(w, sub);
+        const int unit = Group<XT>::unit_of(sub);
+        if (a.qx_tiled) {
+            const int64_t half = ((row / kWaveM) * a.KB + b0 + i) * 8 + (row % kWaveM) / kFragRows * 2 + unit / 4;
+            *reinterpret_cast<uint4 *>(a.qx_tiled + half * kFragBytes + (unit % 4) * 256 + (row % kFragRows) * 16) = out;
+            if (sub == 0) a.x_scale[(int64_t)(b0 + i) * a.Mp + row] = s;
+        } else {
+            const int64_t col = (int64_t)(b0 + i) * kFp8Block + unit * kUnit;
+            uint8_t *const p = a.qx + row * a.K + col;
+            if (col + kUnit <= a.K) {
+                __builtin_memcpy(p, &out, sizeof(out));   // at any alignment
+            } else {
+                const uint32_t v[4] = {out.x, out.y, out.z, out.w};
+                for (int e = 0; e < (int)(a.K - col); ++e) p[e] = (uint8_t)(v[e / 4] >> (8 * (e % 4)));
+            }
+            if (sub == 0) a.x_scale[row * a.KB + b0 + i] = s;
+        }
+    }
+}
+
+// ---- weights ------------------------------------------------------------------------------------
+// A block of threads per 128 x 128 of an expert's matrix: every thread half a row.
+__global__ __launch_bounds__(kThreads) void fp8_pack_kernel(const float *__restrict__ W, int64_t experts, int64_t N, int64_t K,
+                                                            uint8_t *__restrict__ blob, float *__restrict__ w_scale, int64_t NB,
+                                                            int64_t KB, int64_t expert_bytes) {
+    __shared__ float wave_max[kWaves];
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        reinterpret_cast<uint32_t *>(blob)[0] = kFp8PackedTag;
+        int64_t *const h = reinterpret_cast<int64_t *>(blob + 8);
+        h[0] = N; h[1] = K; h[2] = experts;
+    }
+    const int64_t tile = blockIdx.x, b = tile % KB, G = tile / KB % NB, e = tile / KB / NB;
+    const int64_t n = G * kTileN + threadIdx.x / 2, k0 = b * kFp8Block + (threadIdx.x & 1) * kFragK;
+    const float *const wrow = W + (e * N + (n < N ? n : 0)) * K;
+    float v[kFragK];
+    float most = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kFragK; ++j) {
+        v[j] = n < N && k0 + j < K ? wrow[k0 + j] : 0.0f;
+        most = fmaxf(most, fabsf(v[j]));
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+    if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = most;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) most = fmaxf(most, wave_max[w]);
+    const float s = scale_of(most, kE4m3Most);
+    if (threadIdx.x == 0) w_scale[tile] = s;
+    uint8_t *const codes = blob + kPackedHeaderBytes + e * expert_bytes;
+#pragma unroll
+    for (int u = 0; u < kFragK / 16; ++u) {
+        uint32_t w[4];
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+            w[d] = e4m3x4(v[16 * u + 4 * d] / s, v[16 * u + 4 * d + 1] / s, v[16 * u + 4 * d + 2] / s, v[16 * u + 4 * d + 3] / s);
+        *reinterpret_cast<uint4 *>(codes + fp8_weight_offset(n, k0 + 16 * u, KB)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void fp8_unpack_kernel(const uint8_t *__restrict__ codes, int64_t N, int64_t K, int64_t KB,
+                                                              int64_t expert_bytes, int64_t total, uint8_t *__restrict__ out) {
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
+        const int64_t k = i % K, n = i / K % N, e = i / K / N;
+        out[i] = codes[e * expert_bytes + fp8_weight_offset(n, k, KB)];
+    }
+}
+
+}  // namespace
+
+hipError_t launch_fp8_quant(const void *X, qc_dtype xdt, int64_t M, int64_t K, uint8_t *qx, uint8_t *qx_tiled, float *x_scale,
+                            const int32_t *offsets, int experts, int tokens, Fp8Tile *map, hipStream_t stream) {
+    QuantArgs a{};
+    a.X = X;
+    a.qx = qx;
+    a.qx_tiled = qx_tiled;
+    a.x_scale = x_scale;
+    a.M = M;
+    a.K = K;
+    a.Mp = round_up(M, kWaveM);
+    a.KB = (int)fp8_blocks(K);
+    constexpr int G = 3;
+    a.chunks = (a.KB + G - 1) / G;
+    a.quant_blocks = (int)((M + kWaves * kRowsPerWave - 1) / (kWaves * kRowsPerWave) * a.chunks);
+    if (offsets) {
+        a.offsets = offsets;
+        a.map = map;
+        a.experts = experts;
+        a.tokens = tokens;
+        a.map_entries = (int)fp8_tiles_most(M, experts, tokens);
+    }
+    const dim3 grid((unsigned)(a.quant_blocks + (offsets ? 1 : 0))), block(kThreads);
+    if (xdt == QC_BF16) fp8_quant_kernel<uint16_t, G><<<grid, block, 0, stream>>>(a);
+    else fp8_quant_kernel<float, G><<<grid, block, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_fp8_pack(const float *W, int64_t experts, int64_t N, int64_t K, uint8_t *blob, float *w_scale, hipStream_t stream) {
+    const int64_t NB = round_up(N, kTileN) / kTileN, KB = fp8_blocks(K);
+    fp8_pack_kernel<<<dim3((unsigned)(experts * NB * KB)), dim3(kThreads), 0, stream>>>(W, experts, N, K, blob, w_scale, NB, KB,
+                                                                                       fp8_weight_bytes(N, K));
+    return hipGetLastError();
+}
+
+hipError_t launch_fp8_unpack(const uint8_t *blob, int64_t experts, int64_t N, int64_t K, uint8_t *codes, hipStream_t stream) {
+    const int64_t total = experts * N * K, blocks = (total + kThreads - 1) / kThreads;
+    fp8_unpack_kernel<<<dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(kThreads), 0, stream>>>(
+        blob + kPackedHeaderBytes, N, K, fp8_blocks(K), fp8_weight_bytes(N, K), total, codes);
+    return hipGetLastError();
+}
+
+}  // namespace qc
