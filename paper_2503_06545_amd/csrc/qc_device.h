@@ -1,6 +1,8 @@
 // Device helpers shared by the quantization and the GEMM translation units: groups of 128 columns of an
-// activation row, the quantizer's exact quotient and cast, the epilogue's activations.
+// activation row, the quantizer's exact quotient and cast, the GEMMs' copies to LDS, map of tiles and stores, the epilogue's activations.
 #pragma once
+
+#include <type_traits>
 
 #include "qc_internal.h"
 
@@ -325,6 +327,42 @@ struct Rotation {
         return sign;
     }
 };
+
+__device__ inline void lds_dma_16(const uint8_t *gsrc, uint8_t *lds_dst) {
+    __builtin_amdgcn_global_load_lds(
+        (const __attribute__((address_space(1))) void *)gsrc,
+        (__attribute__((address_space(3))) void *)lds_dst, 16, 0, 0);
+}
+
+// Map the launch's block index to a tile so that the blocks resident on one XCD at a time
+// (block b runs on XCD b % 8) work on a compact 8 x 8 patch of tiles and share its operand
+// panels through that XCD's L2.
+__device__ inline void tile_of_block(int b, int nblocks, int m_tiles, int n_tiles, int group_m,
+                                     int &mt, int &nt) {
+    const int xcd = b % 8, slot = b / 8;
+    const int per = nblocks / 8, extra = nblocks % 8;
+    const int v = xcd * per + (xcd < extra ? xcd : extra) + slot;  // blocks of one XCD are consecutive
+    const int kGroupM = group_m;
+    const int per_group = kGroupM * n_tiles;
+    const int g = v / per_group, r = v % per_group;
+    const int m0 = g * kGroupM;
+    const int gm = (m_tiles - m0) < kGroupM ? (m_tiles - m0) : kGroupM;
+    mt = m0 + r % gm;
+    nt = r / gm;
+}
+
+// vmcnt(n) with the other counters left unconstrained (gfx9 encoding: bits 3:0 and 15:14, n < 64)
+#define QC_WAIT_VMCNT(n) __builtin_amdgcn_s_waitcnt(0x0F70 | ((n) & 15) | (((n) >> 4) << 14))
+
+// One piece of a row of Y.  ANY: at any alignment of its elements.  CACHED: not past the caches, where
+// the pieces of a line that two tiles, two rows or two instructions share meet.
+template <bool ANY, bool CACHED, typename T, typename V>
+__device__ inline void store_piece(T *p, V v) {
+    typedef V VAny __attribute__((aligned(2)));
+    typedef std::conditional_t<ANY, VAny, V> P;
+    if constexpr (CACHED) *reinterpret_cast<P *>(p) = v;
+    else __builtin_nontemporal_store(v, reinterpret_cast<P *>(p));
+}
 
 __device__ inline float gelu_tanh_f(float y) {
     // 0.5 y (1 + tanh(u)) = y / (1 + exp(-2u)),  u = sqrt(2/pi) (y + 0.044715 y^3)

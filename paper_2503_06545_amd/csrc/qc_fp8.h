@@ -90,7 +90,7 @@ struct Fp8GemmArgs {
     int KB, m_tiles, n_tiles, group_m;
 };
 
-int fp8_gemm_tokens(int64_t M, int64_t N, int64_t K, int experts);   // of the GEMM's tiles
+int fp8_gemm_tokens(int64_t M, int64_t N, int64_t K, int experts, qc_out ydt);   // of the GEMM's tiles
 hipError_t launch_fp8_gemm(const Fp8GemmArgs &args, int tokens, qc_epilogue epi, qc_out ydt, hipStream_t stream);
 
 }  // namespace qc

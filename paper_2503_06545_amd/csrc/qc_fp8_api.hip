@@ -66,6 +66,7 @@ qc_status gemm(const void *workspace, int64_t M, int64_t K, const void *packed, 
     a.KB = (int)ws.KB;
     a.m_tiles = (int)(grouped ? fp8_tiles_most(M, experts, tokens) : (M + tokens - 1) / tokens);
     a.n_tiles = (int)(round_up(N, kTileN) / kTileN);
+    a.group_m = a.n_tiles > 16 ? 8 : (a.KB >= 18 ? 3 : 2);
     return device_status(launch_fp8_gemm(a, tokens, epi, ydt, (hipStream_t)stream));
 }
 
@@ -123,7 +124,7 @@ extern "C" qc_status qc_qlinear_fp8_gemm(const void *workspace, size_t workspace
     QC_TRY(check_workspace(workspace));
     QC_TRY(check_gemm_supported(M, K, N, 1, ydt));
     if (workspace_bytes < fp8_workspace(M, K).total_bytes) return QC_ERR_WORKSPACE;
-    return gemm(workspace, M, K, packed, w_scale, N, bias, epi, Y, ydt, 1, fp8_gemm_tokens(M, N, K, 1), false, stream);
+    return gemm(workspace, M, K, packed, w_scale, N, bias, epi, Y, ydt, 1, fp8_gemm_tokens(M, N, K, 1, ydt), false, stream);
 }
 
 extern "C" qc_status qc_qlinear_fp8(const void *X, qc_dtype xdt, int64_t M, int64_t K, const void *packed, const float *w_scale,
@@ -154,7 +155,7 @@ extern "C" qc_status qc_qlinear_fp8_grouped(const void *X, qc_dtype xdt, int64_t
     const Fp8Workspace ws = fp8_workspace(M, K);
     if (workspace_bytes < ws.total_bytes) return QC_ERR_WORKSPACE;
     uint8_t *const base = (uint8_t *)workspace;
-    const int tokens = fp8_gemm_tokens(M, N, K, (int)experts);
+    const int tokens = fp8_gemm_tokens(M, N, K, (int)experts, ydt);
     QC_TRY(device_status(launch_fp8_quant(X, xdt, M, K, nullptr, base + ws.codes_offset, (float *)base, expert_offsets, (int)experts,
                                           tokens, (Fp8Tile *)(base + ws.map_offset), (hipStream_t)stream)));
     return gemm(workspace, M, K, packed, w_scale, N, bias, epi, Y, ydt, (int)experts, tokens, true, stream);

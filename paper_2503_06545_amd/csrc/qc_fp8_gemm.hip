@@ -79,51 +79,139 @@ __device__ inline Where tile_of(const Fp8GemmArgs &a, int v, int tokens) {
     return {row0, (int)(rows < tokens ? rows : tokens), 0};
 }
 
-// MI x 16 tokens x 128 channels per wavefront, four wavefronts along the tokens
+constexpr int kSlots = 3;   // of the ring of weights in LDS, a block of 128 k each
+constexpr int kRingBytes = kSlots * kFp8TileBytes;
+
+// A block of four wavefronts computes 64 MI tokens x 128 channels, a wavefront 16 MI of the tokens.  The weights, which
+// all four use, go HBM -> LDS by linear copies through a ring and are read back 16 B a lane; the activations are
+// private to a wavefront and go HBM -> registers, a block of 128 k ahead.  Two blocks fit a CU, so that one's epilogue
+// and waits lie under the other's matrix instructions.
+//
+// Loads and LDS reads are asm so that they stay in flight under counted waits; each wait names the registers that it makes
+// valid.  Vector memory operations complete in order, which is W(0) X(0) W(1) W(2), then X(s + 1) at the start and W(s + 3) in the
+// middle of step s, where X are the activations with their scales.  The wait for X(s), after X(s + 1) has been requested, leaves that
+// and W(s + 2) in flight, so W(s + 1) has landed with it; the barrier in the middle of the step then makes the next
+// step's weights readable and the slot of this one's free, whose last reads are in registers by then.
+// Past the last step the index is clamped: those copies repeat data that is not used again.
 template <int MI, int OUT, int EPI>
-__global__ __launch_bounds__(kThreads) void fp8_tile_kernel(Fp8GemmArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
+    constexpr bool EXACT = OUT == QC_OUT_F32;
+    typedef Operand<EXACT> Op;
     constexpr int TM = 64 * MI;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    float *const lds_bs = reinterpret_cast<float *>(lds + kRingBytes);   // 128 biases
+    float *const lds_sw = lds_bs + kTileN;                               // the channel tile's scales, one for each step
+
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, h = lane >> 4;
-    const int v = blockIdx.x / (uint32_t)a.n_tiles, nt = blockIdx.x % (uint32_t)a.n_tiles;
+    int v, nt;
+    tile_of_block(blockIdx.x, gridDim.x, a.m_tiles, a.n_tiles, a.group_m, v, nt);
     const Where at = tile_of(a, v, TM);
-    const int live = at.rows - wave * (16 * MI);   // rows of this wavefront's tile
-    if (at.expert < 0 || live <= 0) return;
-    const int64_t m0 = at.row0 + wave * (16 * MI);
+    if (at.expert < 0) return;
+    const int first = wave * (16 * MI), live = at.rows - first;   // rows of this wavefront that are stored: may be none
+    const int KB = a.KB, last = KB - 1;
 
-    const uint8_t *const wsrc = a.w_codes + at.expert * a.w_expert_bytes + (int64_t)nt * a.KB * kFp8TileBytes + lane * 16;
-    const float *const ws = a.w_scale + ((int64_t)at.expert * a.n_tiles + nt) * a.KB;
-    // rows past the last live one read that one again and are not stored
-    const uint8_t *xsrc[MI];
-    int64_t xs[MI][4];
+    {
+        const float *const ws = a.w_scale + ((int64_t)at.expert * a.n_tiles + nt) * KB;
+        for (int b = threadIdx.x; b < KB; b += kThreads) lds_sw[b] = ws[b];
+        const int64_t n = (int64_t)nt * kTileN + threadIdx.x;
+        if (threadIdx.x < kTileN) lds_bs[threadIdx.x] = a.bias && n < a.N ? a.bias[at.expert * a.N + n] : 0.0f;
+    }
+    const uint8_t *const wsrc = a.w_codes + at.expert * a.w_expert_bytes + (int64_t)nt * KB * kFp8TileBytes + wave * (4 * kFragBytes) + lane * 16;
+    auto issue_w = [&](int step, int slot) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            lds_dma_16(wsrc + (int64_t)step * kFp8TileBytes + j * kFragBytes, lds + slot * kFp8TileBytes + (wave * 4 + j) * kFragBytes);
+    };
+
+    // Rows past the last live one of the tile read that one again.  A lane's place relative to the panel of 64 tokens that
+    // the tile begins in, and, for the scales of its four rows, relative to its first row (the three floats behind a
+    // row's last scale are other rows' or the codes).
+    const int64_t m0 = at.row0;
+    const uint8_t *const xsrc = a.x_tiled + (m0 / kWaveM) * KB * (8 * kFragBytes);
+    const float *const ssrc = a.x_scale + m0;
+    uint32_t xoff[MI], soff[MI];
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-        const int64_t r = m0 + min(16 * i + c, live - 1);
-        xsrc[i] = a.x_tiled + fp8_act_offset(r, 16 * h, a.KB);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) xs[i][q] = m0 + min(16 * i + 4 * h + q, live - 1);
+        const int r = (int)(m0 % kWaveM) + min(first + 16 * i + c, at.rows - 1);
+        xoff[i] = (uint32_t)((r / kWaveM) * KB * 8 + r % kWaveM / kFragRows * 2) * kFragBytes + h * 256 + r % kFragRows * 16;
+        soff[i] = 4 * min(first + 16 * i + 4 * h, at.rows - 1);
     }
+
+    v4i xq[2][MI][2];
+    f4 sc[2][MI];
+    // (s_nop: a vector instruction may have written the scalar base just before, and the compiler sees no memory instruction)
+#define QC_LOAD_FIRST(dst, off, base) asm volatile("s_nop 4\n\tglobal_load_dwordx4 %0, %1, %2" : "=v"(dst) : "v"(off), "s"(base) : "memory")
+#define QC_LOAD(dst, off, base, imm) asm volatile("global_load_dwordx4 %0, %1, %2 offset:%3" : "=v"(dst) : "v"(off), "s"(base), "n"(imm) : "memory")
+#define QC_ISSUE_X(step, SLOT)                                                  \
+    do {                                                                        \
+        const uint8_t *const p_ = xsrc + (int64_t)(step) * (8 * kFragBytes);    \
+        const float *const q_ = ssrc + (int64_t)(step) * a.Mp;                  \
+        QC_LOAD_FIRST(sc[SLOT][0], soff[0], q_);                                \
+        _Pragma("unroll") for (int i = 1; i < MI; ++i) QC_LOAD(sc[SLOT][i], soff[i], q_, 0); \
+        QC_LOAD_FIRST(xq[SLOT][0][0], xoff[0], p_);                             \
+        QC_LOAD(xq[SLOT][0][1], xoff[0], p_, kFragBytes);                       \
+        _Pragma("unroll") for (int i = 1; i < MI; ++i) {                        \
+            QC_LOAD(xq[SLOT][i][0], xoff[i], p_, 0);                            \
+            QC_LOAD(xq[SLOT][i][1], xoff[i], p_, kFragBytes);                   \
+        }                                                                       \
+    } while (0)
+#define QC_WAIT_X(n, SLOT)                                                                                           \
+    do {                                                                                                             \
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n));                                                                \
+        _Pragma("unroll") for (int i = 0; i < MI; ++i)                                                               \
+            asm volatile("" : "+v"(xq[SLOT][i][0]), "+v"(xq[SLOT][i][1]), "+v"(sc[SLOT][i]));                        \
+    } while (0)
+
+    // weights: wq[t % 4] the channels 8 c + t of the step; read two ahead
+    v4i wq[4][2];
+    float sw;
+    const uint32_t lds_lane = (uint32_t)(uintptr_t)lds + lane * 16, lds_sw_at = (uint32_t)(uintptr_t)lds_sw;
+#define QC_READ_W(base, t)                                                                                      \
+    do {                                                                                                        \
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % 4][0]) : "v"(base), "n"((t) * 2 * kFragBytes));          \
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % 4][1]) : "v"(base), "n"(((t) * 2 + 1) * kFragBytes));    \
+    } while (0)
+#define QC_WAIT_W(n, t) asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(wq[(t) % 4][0]), "+v"(wq[(t) % 4][1]) : "n"(n))
+#define QC_CLAMP(st) ((st) < last ? (st) : last)
+
     f4 acc[MI][8];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int t = 0; t < 8; ++t) acc[i][t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int b = 0; b < a.KB; ++b) {
-        typedef Operand<OUT == QC_OUT_F32> Op;
-        Op x[MI];
+
+    int slot = 0;   // step % 3
+    auto run_step = [&](int step, auto xslot) {
+        constexpr int XS = decltype(xslot)::value;
+        const int next = slot == kSlots - 1 ? 0 : slot + 1;
+        const uint32_t here = lds_lane + slot * kFp8TileBytes, there = lds_lane + next * kFp8TileBytes;
+        asm volatile("ds_read_b32 %0, %1" : "=v"(sw) : "v"(lds_sw_at + 4 * step));
+        QC_ISSUE_X(QC_CLAMP(step + 1), 1 - XS);
+        QC_WAIT_X(4 + 3 * MI, XS);
+        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(sw), "+v"(wq[0][0]), "+v"(wq[0][1]), "+v"(wq[1][0]), "+v"(wq[1][1]));
         float s[MI][4];
-        const float sw = ws[b];
+        Op x[MI];
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
-            const v4i *const p = reinterpret_cast<const v4i *>(xsrc[i] + (int64_t)b * (8 * kFragBytes));
-            x[i] = Op(p[0], p[64]);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) s[i][q] = a.x_scale[b * a.Mp + xs[i][q]] * sw;
+            for (int q = 0; q < 4; ++q) s[i][q] = sc[XS][i][q] * sw;
+            x[i] = Op(xq[XS][i][0], xq[XS][i][1]);
         }
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-            const v4i *const p = reinterpret_cast<const v4i *>(wsrc + (int64_t)b * kFp8TileBytes + 2 * t * kFragBytes);
-            const Op w(p[0], p[64]);
+            if (t < 6) QC_READ_W(here, t + 2);
+            if (t == 6) {   // tiles 6 and 7 are in registers: this wavefront is done with the slot
+                asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(wq[2][0]), "+v"(wq[2][1]), "+v"(wq[3][0]), "+v"(wq[3][1]));
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                issue_w(QC_CLAMP(step + 3), slot);
+                QC_READ_W(there, 0);
+                QC_READ_W(there, 1);
+            } else if (t > 1 && t < 6) {
+                QC_WAIT_W(4, t);
+            }
+            const Op w(wq[t % 4][0], wq[t % 4][1]);
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
                 const f4 p = product(x[i], w);
@@ -131,55 +219,98 @@ __global__ __launch_bounds__(kThreads) void fp8_tile_kernel(Fp8GemmArgs a) {
                 for (int q = 0; q < 4; ++q) acc[i][t][q] = fmaf(p[q], s[i][q], acc[i][t][q]);
             }
         }
-    }
+        slot = next;
+    };
 
+    issue_w(0, 0);
+    QC_ISSUE_X(0, 0);
+    issue_w(QC_CLAMP(1), 1);
+    issue_w(QC_CLAMP(2), 2);
+    QC_WAIT_VMCNT(3 * MI + 8);   // W(0) has landed
+    __syncthreads();             // and everybody else's, with the scales
+    QC_READ_W(lds_lane, 0);
+    QC_READ_W(lds_lane, 1);
+    int step = 0;
+    for (; step + 2 <= KB; step += 2) {
+        run_step(step, std::integral_constant<int, 0>{});
+        run_step(step + 1, std::integral_constant<int, 1>{});
+    }
+    if (step < KB) run_step(step, std::integral_constant<int, 0>{});
+    // drain what is in flight before its registers are used for anything else
+    QC_WAIT_X(0, 0);
+    QC_WAIT_X(0, 1);
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(wq[0][0]), "+v"(wq[0][1]), "+v"(wq[1][0]), "+v"(wq[1][1]));
+#undef QC_CLAMP
+#undef QC_WAIT_W
+#undef QC_READ_W
+#undef QC_WAIT_X
+#undef QC_ISSUE_X
+#undef QC_LOAD
+#undef QC_LOAD_FIRST
+
+    // ---- epilogue: lane (c, h) holds channels 8 c .. + 7 of tokens 16 i + 4 h + q
     const int64_t n0 = (int64_t)nt * kTileN + 8 * c;
-    if (n0 >= a.N) return;
-    const int cols = (int)(a.N - n0 < 8 ? a.N - n0 : 8);
+    constexpr int kOutBytes = OUT == QC_OUT_BF16 ? 2 : 4;
+    const bool whole = live >= 16 * MI && (int64_t)(nt + 1) * kTileN <= a.N && a.N % (16 / kOutBytes) == 0;
     float bs[8];
 #pragma unroll
-    for (int t = 0; t < 8; ++t) bs[t] = a.bias && t < cols ? a.bias[at.expert * a.N + n0 + t] : 0.0f;
+    for (int t = 0; t < 8; ++t) bs[t] = lds_bs[8 * c + t];
+    auto write_tile = [&](auto checked_tag) {
+        constexpr bool CHECKED = decltype(checked_tag)::value;
+        if (CHECKED && n0 >= a.N) return;
+        const int cols = CHECKED ? (int)(a.N - n0 < 8 ? a.N - n0 : 8) : 8;
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (16 * i + 4 * h + q >= live) continue;
-            const int64_t y0 = (m0 + 16 * i + 4 * h + q) * a.N + n0;
-            float y[8];
+            for (int q = 0; q < 4; ++q) {
+                if (CHECKED && 16 * i + 4 * h + q >= live) continue;
+                const int64_t y0 = (m0 + first + 16 * i + 4 * h + q) * a.N + n0;
+                float y[8];
 #pragma unroll
-            for (int t = 0; t < 8; ++t) y[t] = activation<EPI>(acc[i][t][q] + bs[t]);
-            if (OUT == QC_OUT_F32) {
-                float *const p = reinterpret_cast<float *>(a.Y) + y0;
-                if (cols == 8) __builtin_memcpy(p, y, sizeof(y));
-                else for (int t = 0; t < 8; ++t) if (t < cols) p[t] = y[t];
-            } else {
-                uint16_t *const p = reinterpret_cast<uint16_t *>(a.Y) + y0;
-                uint32_t pk[4];
+                for (int t = 0; t < 8; ++t) y[t] = activation<EPI>(acc[i][t][q] + bs[t]);
+                if constexpr (OUT == QC_OUT_F32) {
+                    float *const p = reinterpret_cast<float *>(a.Y) + y0;
+                    if (cols >= 4) store_piece<CHECKED, true>(p, f4{y[0], y[1], y[2], y[3]});
+                    if (cols == 8) store_piece<CHECKED, true>(p + 4, f4{y[4], y[5], y[6], y[7]});
+                    if (CHECKED && cols < 8) {
 #pragma unroll
-                for (int t = 0; t < 4; ++t) pk[t] = pack_bf16x2(y[2 * t], y[2 * t + 1]);
-                if (cols == 8) __builtin_memcpy(p, pk, sizeof(pk));
-                else
+                        for (int t = 0; t < 8; ++t) if (t >= (cols & 4) && t < cols) p[t] = y[t];
+                    }
+                } else {
+                    uint16_t *const p = reinterpret_cast<uint16_t *>(a.Y) + y0;
+                    u32x4 pk;
 #pragma unroll
-                    for (int t = 0; t < 8; ++t) if (t < cols) p[t] = (uint16_t)(t % 2 ? pk[t / 2] >> 16 : pk[t / 2]);
+                    for (int t = 0; t < 4; ++t) pk[t] = pack_bf16x2(y[2 * t], y[2 * t + 1]);
+                    if (cols == 8) store_piece<CHECKED, CHECKED>(p, pk);
+                    else {
+#pragma unroll
+                        for (int t = 0; t < 8; ++t) if (t < cols) p[t] = (uint16_t)(t % 2 ? pk[t / 2] >> 16 : pk[t / 2]);
+                    }
+                }
             }
-        }
+    };
+    if (whole) write_tile(std::false_type{});
+    else write_tile(std::true_type{});
 }
 
-template <int OUT>
-hipError_t launch_out(const Fp8GemmArgs &a, qc_epilogue epi, hipStream_t stream) {
+template <int MI, int OUT>
+hipError_t launch_tiles(const Fp8GemmArgs &a, qc_epilogue epi, hipStream_t stream) {
+    const int bytes = kRingBytes + (kTileN + a.KB) * (int)sizeof(float);
+    static_assert(kRingBytes + (kTileN + QC_MAX_K / kFp8Block) * sizeof(float) <= 64 * 1024, "dynamic LDS beyond the default limit needs an attribute");
     const dim3 grid((unsigned)(a.m_tiles * a.n_tiles)), block(kThreads);
-    if (epi == QC_EPI_GELU_TANH) fp8_tile_kernel<2, OUT, QC_EPI_GELU_TANH><<<grid, block, 0, stream>>>(a);
-    else if (epi == QC_EPI_GELU_ERF) fp8_tile_kernel<2, OUT, QC_EPI_GELU_ERF><<<grid, block, 0, stream>>>(a);
-    else fp8_tile_kernel<2, OUT, QC_EPI_NONE><<<grid, block, 0, stream>>>(a);
+    if (epi == QC_EPI_GELU_TANH) fp8_ring_kernel<MI, OUT, QC_EPI_GELU_TANH><<<grid, block, bytes, stream>>>(a);
+    else if (epi == QC_EPI_GELU_ERF) fp8_ring_kernel<MI, OUT, QC_EPI_GELU_ERF><<<grid, block, bytes, stream>>>(a);
+    else fp8_ring_kernel<MI, OUT, QC_EPI_NONE><<<grid, block, bytes, stream>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-int fp8_gemm_tokens(int64_t M, int64_t N, int64_t K, int experts) { return 128; }
+int fp8_gemm_tokens(int64_t M, int64_t N, int64_t K, int experts, qc_out ydt) { return ydt == QC_OUT_F32 ? 128 : 192; }
 
 hipError_t launch_fp8_gemm(const Fp8GemmArgs &args, int tokens, qc_epilogue epi, qc_out ydt, hipStream_t stream) {
-    return ydt == QC_OUT_F32 ? launch_out<QC_OUT_F32>(args, epi, stream) : launch_out<QC_OUT_BF16>(args, epi, stream);
+    if (ydt == QC_OUT_F32) return launch_tiles<2, QC_OUT_F32>(args, epi, stream);
+    return launch_tiles<3, QC_OUT_BF16>(args, epi, stream);
 }
 
 }  // namespace qc

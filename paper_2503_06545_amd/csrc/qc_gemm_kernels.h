@@ -52,42 +52,6 @@ template <int BITS, bool SPLIT>
 constexpr int kRingBytes = !SPLIT ? kStages * StageLayout<BITS>::kBytes
                            : 2 * kStages * StageLayout<BITS>::kBytes > kSplitThreads * 64 ? 2 * kStages * StageLayout<BITS>::kBytes : kSplitThreads * 64;
 
-__device__ inline void lds_dma_16(const uint8_t *gsrc, uint8_t *lds_dst) {
-    __builtin_amdgcn_global_load_lds(
-        (const __attribute__((address_space(1))) void *)gsrc,
-        (__attribute__((address_space(3))) void *)lds_dst, 16, 0, 0);
-}
-
-// Map the launch's block index to a tile so that the blocks resident on one XCD at a time
-// (block b runs on XCD b % 8) work on a compact 8 x 8 patch of tiles and share its operand
-// panels through that XCD's L2.
-__device__ inline void tile_of_block(int b, int nblocks, int m_tiles, int n_tiles, int group_m,
-                                     int &mt, int &nt) {
-    const int xcd = b % 8, slot = b / 8;
-    const int per = nblocks / 8, extra = nblocks % 8;
-    const int v = xcd * per + (xcd < extra ? xcd : extra) + slot;  // blocks of one XCD are consecutive
-    const int kGroupM = group_m;
-    const int per_group = kGroupM * n_tiles;
-    const int g = v / per_group, r = v % per_group;
-    const int m0 = g * kGroupM;
-    const int gm = (m_tiles - m0) < kGroupM ? (m_tiles - m0) : kGroupM;
-    mt = m0 + r % gm;
-    nt = r / gm;
-}
-
-// vmcnt(n) with the other counters left unconstrained (gfx9 encoding: bits 3:0 and 15:14, n < 64)
-#define QC_WAIT_VMCNT(n) __builtin_amdgcn_s_waitcnt(0x0F70 | ((n) & 15) | (((n) >> 4) << 14))
-
-// One piece of a row of Y.  ANY: at any alignment of its elements.  CACHED: not past the caches, where
-// the pieces of a line that two tiles, two rows or two instructions share meet.
-template <bool ANY, bool CACHED, typename T, typename V>
-__device__ inline void store_piece(T *p, V v) {
-    typedef V VAny __attribute__((aligned(2)));
-    typedef std::conditional_t<ANY, VAny, V> P;
-    if constexpr (CACHED) *reinterpret_cast<P *>(p) = v;
-    else __builtin_nontemporal_store(v, reinterpret_cast<P *>(p));
-}
-
 // Epilogue of one wavefront's tile of 16 MI tokens x 128 channels: registers -> Y.  Lane (c = lane % 16, h = lane / 16)
 // of MFMA tile (i, t) holds, in register r, token m_wave + 16 i + 4 h + r and channel
 // 128 nt + 8 c + t.  sx64 / cx64: the tile's token scales / corrections, lds_sw / lds_bs /
