@@ -87,12 +87,18 @@ constexpr int kRingBytes = kSlots * kFp8TileBytes;
 // private to a wavefront and go HBM -> registers, a block of 128 k ahead.  Two blocks fit a CU, so that one's epilogue
 // and waits lie under the other's matrix instructions.
 //
-// Loads and LDS reads are asm so that they stay in flight under counted waits; each wait names the registers that it makes
-// valid.  Vector memory operations complete in order, which is W(0) X(0) W(1) W(2), then X(s + 1) at the start and W(s + 3) in the
-// middle of step s, where X are the activations with their scales.  The wait for X(s), after X(s + 1) has been requested, leaves that
-// and W(s + 2) in flight, so W(s + 1) has landed with it; the barrier in the middle of the step then makes the next
-// step's weights readable and the slot of this one's free, whose last reads are in registers by then.
+// Loads, copies and LDS reads are asm so that they stay in flight under counted waits; each wait names the registers that it
+// makes valid.  Vector memory operations complete in order, which is the scales and biases, W(0) X(0) W(1) W(2), then X(s + 1)
+// at the start and W(s + 3) towards the end of step s, where X are the activations with their scales.  The wait for X(s), after X(s + 1)
+// has been requested, leaves that and W(s + 2) in flight, so W(s + 1) has landed with it; the barrier before channel
+// block 6 then makes the next step's weights readable and the slot of this one's free, whose last reads are in registers by then.
 // Past the last step the index is clamped: those copies repeat data that is not used again.
+//
+// What bounds it on large problems is power: 8192 x 8192 x 8192 runs at 1.7 of 2.4 GHz with the matrix units 60 % busy, where a
+// loop on registers alone, each product scaled and added, holds 1.9 GHz, 94 % and 3760 TFLOP/s.  us for 131072 x 1152 x 4608,
+// 65536 x 4608 x 1152, 8192 x 8192 x 8192: products scaled at once 737 341 498, three products later 729 339 485; scales
+// through LDS and copies with scalar addresses 702 326 475, with the channel tile's scales loaded ordinarily, a
+// memory round trip ahead of the first copy, 788 329 478.
 template <int MI, int OUT, int EPI>
 __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
     constexpr bool EXACT = OUT == QC_OUT_F32;
@@ -100,7 +106,7 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
     constexpr int TM = 64 * MI;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     float *const lds_bs = reinterpret_cast<float *>(lds + kRingBytes);   // 128 biases
-    float *const lds_sw = lds_bs + kTileN;                               // the channel tile's scales, one for each step
+    float *const lds_sw = lds_bs + kTileN;                               // the channel tile's scales, one for each step, in whole 256
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, h = lane >> 4;
@@ -111,44 +117,51 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
     const int first = wave * (16 * MI), live = at.rows - first;   // rows of this wavefront that are stored: may be none
     const int KB = a.KB, last = KB - 1;
 
-    {
-        const float *const ws = a.w_scale + ((int64_t)at.expert * a.n_tiles + nt) * KB;
-        for (int b = threadIdx.x; b < KB; b += kThreads) lds_sw[b] = ws[b];
-        const int64_t n = (int64_t)nt * kTileN + threadIdx.x;
-        if (threadIdx.x < kTileN) lds_bs[threadIdx.x] = a.bias && n < a.N ? a.bias[at.expert * a.N + n] : 0.0f;
-    }
-    const uint8_t *const wsrc = a.w_codes + at.expert * a.w_expert_bytes + (int64_t)nt * KB * kFp8TileBytes + wave * (4 * kFragBytes) + lane * 16;
+    const uint8_t *const wsrc = a.w_codes + at.expert * a.w_expert_bytes + (int64_t)nt * KB * kFp8TileBytes + wave * (4 * kFragBytes);
+    const uint32_t lane16 = lane * 16;
+    // Copies to LDS as asm, like the loads below: scalar addresses and one 32-bit offset a lane, because vector registers are
+    // short.  Lane l's piece goes to m0 + offset + its size times l; the offset counts on both sides.
+    // (s_nop: a vector instruction may have written the scalar base just before, and the compiler sees no memory instruction.)
+#define QC_COPY_16x4(at_lds, off, base)                                                                        \
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024\n\t" \
+                 "global_load_lds_dwordx4 %1, %2 offset:2048\n\tglobal_load_lds_dwordx4 %1, %2 offset:3072" ::"s"(at_lds), "v"(off), "s"(base) : "memory")
+#define QC_COPY_4(at_lds, off, base) \
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, %2" ::"s"(at_lds), "v"(off), "s"(base) : "memory")
+    const uint32_t lds_ring = (uint32_t)(uintptr_t)lds;
     auto issue_w = [&](int step, int slot) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            lds_dma_16(wsrc + (int64_t)step * kFp8TileBytes + j * kFragBytes, lds + slot * kFp8TileBytes + (wave * 4 + j) * kFragBytes);
+        QC_COPY_16x4(lds_ring + slot * kFp8TileBytes + wave * (4 * kFragBytes), lane16, wsrc + (int64_t)step * kFp8TileBytes);
     };
 
+    // the channel tile's scales and biases, without a wait of their own: ahead of the first weights
+    for (int b = wave * 64; b < KB; b += kThreads)
+        QC_COPY_4((uint32_t)(uintptr_t)(lds_sw + b), 4u * min(b + lane, last), a.w_scale + ((int64_t)at.expert * a.n_tiles + nt) * KB);
+    if (wave < 2) {
+        const int n = nt * kTileN + wave * 64;
+        if (a.bias) QC_COPY_4((uint32_t)(uintptr_t)(lds_bs + wave * 64), 4u * min(lane, max((int)a.N - 1 - n, 0)), a.bias + (at.expert * a.N + min(n, (int)a.N - 1)));
+        else lds_bs[wave * 64 + lane] = 0.0f;
+    }
+
     // Rows past the last live one of the tile read that one again.  A lane's place relative to the panel of 64 tokens that
-    // the tile begins in, and, for the scales of its four rows, relative to its first row (the three floats behind a
-    // row's last scale are other rows' or the codes).
+    // the tile begins in.
     const int64_t m0 = at.row0;
     const uint8_t *const xsrc = a.x_tiled + (m0 / kWaveM) * KB * (8 * kFragBytes);
-    const float *const ssrc = a.x_scale + m0;
-    uint32_t xoff[MI], soff[MI];
+    uint32_t xoff[MI];
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
         const int r = (int)(m0 % kWaveM) + min(first + 16 * i + c, at.rows - 1);
         xoff[i] = (uint32_t)((r / kWaveM) * KB * 8 + r % kWaveM / kFragRows * 2) * kFragBytes + h * 256 + r % kFragRows * 16;
-        soff[i] = 4 * min(first + 16 * i + 4 * h, at.rows - 1);
     }
+    const float *const ssrc = a.x_scale + m0;
+    const uint32_t soff = 4 * min(first + lane, at.rows - 1);
+    const uint32_t lds_sx = (uint32_t)(uintptr_t)(lds_sw + round_up(KB, kThreads)) + wave * (4 * kWaveM);   // 64 scales of this wavefront's, for two steps
 
     v4i xq[2][MI][2];
-    f4 sc[2][MI];
-    // (s_nop: a vector instruction may have written the scalar base just before, and the compiler sees no memory instruction)
 #define QC_LOAD_FIRST(dst, off, base) asm volatile("s_nop 4\n\tglobal_load_dwordx4 %0, %1, %2" : "=v"(dst) : "v"(off), "s"(base) : "memory")
 #define QC_LOAD(dst, off, base, imm) asm volatile("global_load_dwordx4 %0, %1, %2 offset:%3" : "=v"(dst) : "v"(off), "s"(base), "n"(imm) : "memory")
 #define QC_ISSUE_X(step, SLOT)                                                  \
     do {                                                                        \
         const uint8_t *const p_ = xsrc + (int64_t)(step) * (8 * kFragBytes);    \
-        const float *const q_ = ssrc + (int64_t)(step) * a.Mp;                  \
-        QC_LOAD_FIRST(sc[SLOT][0], soff[0], q_);                                \
-        _Pragma("unroll") for (int i = 1; i < MI; ++i) QC_LOAD(sc[SLOT][i], soff[i], q_, 0); \
+        QC_COPY_4(lds_sx + (SLOT) * (16 * kWaveM), soff, ssrc + (int64_t)(step) * a.Mp); \
         QC_LOAD_FIRST(xq[SLOT][0][0], xoff[0], p_);                             \
         QC_LOAD(xq[SLOT][0][1], xoff[0], p_, kFragBytes);                       \
         _Pragma("unroll") for (int i = 1; i < MI; ++i) {                        \
@@ -158,23 +171,25 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
     } while (0)
 #define QC_WAIT_X(n, SLOT)                                                                                           \
     do {                                                                                                             \
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n));                                                                \
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");                                                     \
         _Pragma("unroll") for (int i = 0; i < MI; ++i)                                                               \
-            asm volatile("" : "+v"(xq[SLOT][i][0]), "+v"(xq[SLOT][i][1]), "+v"(sc[SLOT][i]));                        \
+            asm volatile("" : "+v"(xq[SLOT][i][0]), "+v"(xq[SLOT][i][1]));                                           \
     } while (0)
+    constexpr int kXLoads = 2 * MI + 1;
 
-    // weights: wq[t % 4] the channels 8 c + t of the step; read two ahead
-    v4i wq[4][2];
-    float sw;
-    const uint32_t lds_lane = (uint32_t)(uintptr_t)lds + lane * 16, lds_sw_at = (uint32_t)(uintptr_t)lds_sw;
+    // weights: wq[t % 3] the channels 8 c + t of the step; read two ahead, across the end of a step one
+    v4i wq[3][2];
+    const uint32_t lds_lane = lds_ring + lane16, lds_sw_at = (uint32_t)(uintptr_t)lds_sw;
+    const uint32_t lds_sx_lane = lds_sx + h * 16;
 #define QC_READ_W(base, t)                                                                                      \
     do {                                                                                                        \
-        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % 4][0]) : "v"(base), "n"((t) * 2 * kFragBytes));          \
-        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % 4][1]) : "v"(base), "n"(((t) * 2 + 1) * kFragBytes));    \
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % 3][0]) : "v"(base), "n"((t) * 2 * kFragBytes));          \
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % 3][1]) : "v"(base), "n"(((t) * 2 + 1) * kFragBytes));    \
     } while (0)
-#define QC_WAIT_W(n, t) asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(wq[(t) % 4][0]), "+v"(wq[(t) % 4][1]) : "n"(n))
+#define QC_WAIT_W(n, t) asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(wq[(t) % 3][0]), "+v"(wq[(t) % 3][1]) : "n"(n))
 #define QC_CLAMP(st) ((st) < last ? (st) : last)
 
+    constexpr int kDeep = EXACT ? 1 : 3;
     f4 acc[MI][8];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
@@ -186,39 +201,54 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
         constexpr int XS = decltype(xslot)::value;
         const int next = slot == kSlots - 1 ? 0 : slot + 1;
         const uint32_t here = lds_lane + slot * kFp8TileBytes, there = lds_lane + next * kFp8TileBytes;
-        asm volatile("ds_read_b32 %0, %1" : "=v"(sw) : "v"(lds_sw_at + 4 * step));
-        QC_ISSUE_X(QC_CLAMP(step + 1), 1 - XS);
-        QC_WAIT_X(4 + 3 * MI, XS);
-        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(sw), "+v"(wq[0][0]), "+v"(wq[0][1]), "+v"(wq[1][0]), "+v"(wq[1][1]));
-        float s[MI][4];
+        f4 sc[MI];
+        float sw;
         Op x[MI];
+        QC_ISSUE_X(QC_CLAMP(step + 1), 1 - XS);
+        QC_WAIT_X(4 + kXLoads, XS);
+        asm volatile("ds_read_b32 %0, %1" : "=v"(sw) : "v"(lds_sw_at + 4 * step));
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
+        for (int i = 0; i < MI; ++i)
+            asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(sc[i]) : "v"(lds_sx_lane), "n"(XS * 16 * kWaveM + 64 * i));
 #pragma unroll
-            for (int q = 0; q < 4; ++q) s[i][q] = sc[XS][i][q] * sw;
-            x[i] = Op(xq[XS][i][0], xq[XS][i][1]);
-        }
+        for (int i = 0; i < MI; ++i) x[i] = Op(xq[XS][i][0], xq[XS][i][1]);
+        // The products' way through the matrix unit lies under the next ones: one is scaled kDeep products later.
+        f4 p[kDeep + 1];
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            if (t < 6) QC_READ_W(here, t + 2);
-            if (t == 6) {   // tiles 6 and 7 are in registers: this wavefront is done with the slot
-                asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(wq[2][0]), "+v"(wq[2][1]), "+v"(wq[3][0]), "+v"(wq[3][1]));
-                __builtin_amdgcn_s_barrier();
-                asm volatile("" ::: "memory");
-                issue_w(QC_CLAMP(step + 3), slot);
-                QC_READ_W(there, 0);
-                QC_READ_W(there, 1);
-            } else if (t > 1 && t < 6) {
-                QC_WAIT_W(4, t);
+        for (int n = 0; n < 8 * MI + kDeep; ++n) {
+            const int t = n / MI, i = n % MI;
+            if (i == 0 && t < 8) {
+                if (t < 6) QC_READ_W(here, t + 2);
+                if (t == 0) QC_WAIT_W(2 + MI + 1 + 2, 0);
+                else if (t == 6) {   // tiles 6 and 7 are in registers: this wavefront is done with the slot
+                    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(wq[0][0]), "+v"(wq[0][1]), "+v"(wq[1][0]), "+v"(wq[1][1]));
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    issue_w(QC_CLAMP(step + 3), slot);
+                } else if (t == 7) {
+                    QC_READ_W(there, 0);
+                } else {
+                    QC_WAIT_W(4, t);
+                }
             }
-            const Op w(wq[t % 4][0], wq[t % 4][1]);
+            if (t < 8) p[n % (kDeep + 1)] = product(x[i], Op(wq[t % 3][0], wq[t % 3][1]));
+            __builtin_amdgcn_sched_barrier(0);
+            if (n == kDeep) {
+                asm volatile("s_waitcnt lgkmcnt(2)" : "+v"(sw));
 #pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const f4 p = product(x[i], w);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) acc[i][t][q] = fmaf(p[q], s[i][q], acc[i][t][q]);
+                for (int j = 0; j < MI; ++j) {
+                    asm volatile("" : "+v"(sc[j]));
+                    sc[j] *= sw;
+                }
             }
+            if (n >= kDeep) {
+                const int to = (n - kDeep) / MI, io = (n - kDeep) % MI;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc[io][to][q] = fmaf(p[(n - kDeep) % (kDeep + 1)][q], sc[io][q], acc[io][to][q]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
+        QC_READ_W(there, 1);
         slot = next;
     };
 
@@ -226,7 +256,7 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
     QC_ISSUE_X(0, 0);
     issue_w(QC_CLAMP(1), 1);
     issue_w(QC_CLAMP(2), 2);
-    QC_WAIT_VMCNT(3 * MI + 8);   // W(0) has landed
+    QC_WAIT_VMCNT(kXLoads + 8);   // W(0) has landed
     __syncthreads();             // and everybody else's, with the scales
     QC_READ_W(lds_lane, 0);
     QC_READ_W(lds_lane, 1);
@@ -247,6 +277,8 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
 #undef QC_ISSUE_X
 #undef QC_LOAD
 #undef QC_LOAD_FIRST
+#undef QC_COPY_4
+#undef QC_COPY_16x4
 
     // ---- epilogue: lane (c, h) holds channels 8 c .. + 7 of tokens 16 i + 4 h + q
     const int64_t n0 = (int64_t)nt * kTileN + 8 * c;
@@ -295,8 +327,8 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
 
 template <int MI, int OUT>
 hipError_t launch_tiles(const Fp8GemmArgs &a, qc_epilogue epi, hipStream_t stream) {
-    const int bytes = kRingBytes + (kTileN + a.KB) * (int)sizeof(float);
-    static_assert(kRingBytes + (kTileN + QC_MAX_K / kFp8Block) * sizeof(float) <= 64 * 1024, "dynamic LDS beyond the default limit needs an attribute");
+    const int bytes = kRingBytes + (int)(kTileN + round_up(a.KB, kThreads) + 2 * 4 * kWaveM) * (int)sizeof(float);
+    static_assert(kRingBytes + (kTileN + QC_MAX_K / kFp8Block + 2 * 4 * kWaveM) * sizeof(float) <= 64 * 1024, "dynamic LDS beyond the default limit needs an attribute");
     const dim3 grid((unsigned)(a.m_tiles * a.n_tiles)), block(kThreads);
     if (epi == QC_EPI_GELU_TANH) fp8_ring_kernel<MI, OUT, QC_EPI_GELU_TANH><<<grid, block, bytes, stream>>>(a);
     else if (epi == QC_EPI_GELU_ERF) fp8_ring_kernel<MI, OUT, QC_EPI_GELU_ERF><<<grid, block, bytes, stream>>>(a);
