@@ -42,7 +42,7 @@ EXPORTS = (
     "qc_qlinear_tensor_workspace_bytes", "qc_qlinear_tensor", "qc_latent_delta_static",
     "qc_packed_weight_fp8_bytes", "qc_pack_weight_fp8", "qc_unpack_weight_codes_fp8", "qc_quant_act_fp8",
     "qc_qlinear_fp8_workspace_bytes", "qc_qlinear_fp8", "qc_qlinear_fp8_quant", "qc_qlinear_fp8_gemm",
-    "qc_qlinear_fp8_grouped",
+    "qc_qlinear_fp8_grouped", "qc_debug_linear_plan_fp8",
 )
 
 
@@ -168,6 +168,8 @@ def lib() -> ctypes.CDLL:
         L.qc_qlinear_fp8_gemm.argtypes = [vp, sz, i64, i64, vp, vp, i64, vp, i32, vp, i32, vp]
         L.qc_qlinear_fp8_grouped.restype = i32
         L.qc_qlinear_fp8_grouped.argtypes = [vp, i32, i64, i64, vp, i64, vp, vp, i64, vp, i32, vp, i32, vp, sz, vp]
+        L.qc_debug_linear_plan_fp8.restype = i32
+        L.qc_debug_linear_plan_fp8.argtypes = [i64, i64, i64, i64, i32, vp]
         L.qc_divergence_score.restype = f32
         L.qc_divergence_score.argtypes = [f32, i32, f32]
         L.qc_cache_interval.restype = i32
@@ -415,6 +417,19 @@ def qc_qlinear_fp8_grouped(X, xdt, M, K, expert_offsets, experts, packed, w_scal
                            workspace_bytes, stream=0) -> int:
     return int(lib().qc_qlinear_fp8_grouped(X, xdt, M, K, expert_offsets, experts, packed, w_scale, N, bias, epi, Y, ydt,
                                             workspace, workspace_bytes, stream))
+
+
+def qc_debug_linear_plan_fp8(M, K, N, experts, ydt, plan) -> int:
+    return int(lib().qc_debug_linear_plan_fp8(M, K, N, experts, ydt, plan))
+
+
+def linear_plan_fp8(M: int, K: int, N: int, out: str = "bf16", experts: int = 0) -> dict:
+    """What an 8-bit floating-point linear's launches are (host only): kernel "ring" or "few", tokens and channels of its tiles,
+    and whether the quantization is fused; experts: of a grouped one."""
+    plan = (ctypes.c_int32 * 4)()
+    if qc_debug_linear_plan_fp8(M, K, N, experts, OUT[out], ctypes.cast(plan, ctypes.c_void_p)) != 0:
+        raise QcError(QC_ERR_INVALID_ARG, "qc_debug_linear_plan_fp8")
+    return {"kernel": (None, "ring", None, "few")[plan[0]], "tokens": plan[1], "channels": plan[2], "fused": bool(plan[3])}
 
 
 def qc_frame_gradient_norm_workspace_bytes(frames: int, inner: int) -> int:

@@ -20,7 +20,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqc.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["qc_api.hip", "qc_quant.hip", "qc_pack.hip", "qc_gemm.hip", "qc_gemm_w8.hip", "qc_gemm_w4.hip", "qc_small.hip", "qc_delta.hip",
-           "qc_fp8_api.hip", "qc_fp8_quant.hip", "qc_fp8_gemm.hip"]
+           "qc_fp8_api.hip", "qc_fp8_quant.hip", "qc_fp8_gemm.hip", "qc_fp8_few.hip"]
 ROOFS_SRC = os.path.join(ROOT, "bench", "qc_roofs.hip")
 ROOFS = os.path.join(ROOT, "bench", "qc_roofs")  # stand-alone roofline micro-benchmark
 TORCH_SRC = os.path.join(CSRC, "qc_torch.cpp")   # the per-step tensor helpers, host code

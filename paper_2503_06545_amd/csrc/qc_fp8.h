@@ -71,7 +71,8 @@ __host__ inline Fp8Workspace fp8_workspace(int64_t M, int64_t K) {
 // ---- launchers ----------------------------------------------------------------------------
 
 // Codes row major with scales [M, KB] (qx), or in the GEMM's order with scales [KB, Mp] (qx_tiled).  offsets: of a grouped
-// linear, device int32 [experts + 1]: the map of its tiles of `tokens` rows is made too, and rows of no group are passed over.
+// linear, device int32 [experts + 1]: rows of no group are passed over, and the map of its tiles of `tokens` rows is made if
+// there is one.
 hipError_t launch_fp8_quant(const void *X, qc_dtype xdt, int64_t M, int64_t K, uint8_t *qx, uint8_t *qx_tiled, float *x_scale,
                             const int32_t *offsets, int experts, int tokens, Fp8Tile *map, hipStream_t stream);
 
@@ -79,18 +80,32 @@ hipError_t launch_fp8_pack(const float *W, int64_t experts, int64_t N, int64_t K
 hipError_t launch_fp8_unpack(const uint8_t *blob, int64_t experts, int64_t N, int64_t K, uint8_t *codes, hipStream_t stream);
 
 struct Fp8GemmArgs {
-    const uint8_t *x_tiled;
-    const float *x_scale;
+    uint8_t *x_tiled;
+    float *x_scale;
     const uint8_t *w_codes;
     const float *w_scale;
     const float *bias;
     void *Y;
-    const Fp8Tile *map;     // grouped; null: one weight, tiles in order
+    Fp8Tile *map;           // grouped; null: one weight, tiles in order
     int64_t M, N, Mp, w_expert_bytes;
     int KB, m_tiles, n_tiles, group_m;
 };
 
-int fp8_gemm_tokens(int64_t M, int64_t N, int64_t K, int experts, qc_out ydt);   // of the GEMM's tiles
+// The kernels for few tokens (qc_fp8_few.hip): 16, 32 or 64 tokens by 16 times 1, 2 or 4 channels
+struct Fp8FewTile {
+    int tokens, frags;   // tokens 0: not for these sizes
+};
+// how a linear of these sizes, or a grouped one with so many experts, goes out
+struct Fp8Plan {
+    bool fused;       // quantization and products in one launch, of the few-token kernel
+    Fp8FewTile few;
+    int tokens;       // of the tiles, whatever the kernel
+};
+Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, int experts, bool grouped, qc_out ydt, bool may_fuse);
+// X null: from the codes and scales that args names, without offsets
+hipError_t launch_fp8_few(const void *X, qc_dtype xdt, int64_t K, const int32_t *offsets, int experts, const Fp8GemmArgs &args,
+                          Fp8FewTile tile, qc_epilogue epi, qc_out ydt, hipStream_t stream);
+
 hipError_t launch_fp8_gemm(const Fp8GemmArgs &args, int tokens, qc_epilogue epi, qc_out ydt, hipStream_t stream);
 
 }  // namespace qc

@@ -47,27 +47,46 @@ qc_status check_gemm_supported(int64_t M, int64_t K, int64_t N, int64_t experts,
 
 qc_status check_workspace(const void *workspace) { return workspace && aligned(workspace, 256) ? QC_OK : QC_ERR_INVALID_ARG; }
 
-qc_status gemm(const void *workspace, int64_t M, int64_t K, const void *packed, const float *w_scale, int64_t N, const float *bias,
-               qc_epilogue epi, void *Y, qc_out ydt, int experts, int tokens, bool grouped, void *stream) {
+Fp8GemmArgs gemm_args(void *workspace, int64_t M, int64_t K, const void *packed, const float *w_scale, int64_t N, const float *bias,
+                      void *Y, const Fp8Plan &plan, int64_t experts, bool grouped) {
     const Fp8Workspace ws = fp8_workspace(M, K);
-    const uint8_t *const base = (const uint8_t *)workspace;
+    uint8_t *const base = (uint8_t *)workspace;
     Fp8GemmArgs a{};
     a.x_tiled = base + ws.codes_offset;
-    a.x_scale = (const float *)base;
+    a.x_scale = (float *)base;
     a.w_codes = (const uint8_t *)packed + kPackedHeaderBytes;
     a.w_scale = w_scale;
     a.bias = bias;
     a.Y = Y;
-    a.map = grouped ? (const Fp8Tile *)(base + ws.map_offset) : nullptr;
+    a.map = grouped && !plan.few.tokens ? (Fp8Tile *)(base + ws.map_offset) : nullptr;
     a.M = M;
     a.N = N;
     a.Mp = ws.Mp;
     a.w_expert_bytes = fp8_weight_bytes(N, K);
     a.KB = (int)ws.KB;
-    a.m_tiles = (int)(grouped ? fp8_tiles_most(M, experts, tokens) : (M + tokens - 1) / tokens);
+    a.m_tiles = (int)(grouped ? fp8_tiles_most(M, experts, plan.tokens) : (M + plan.tokens - 1) / plan.tokens);
     a.n_tiles = (int)(round_up(N, kTileN) / kTileN);
     a.group_m = a.n_tiles > 16 ? 8 : (a.KB >= 18 ? 3 : 2);
-    return device_status(launch_fp8_gemm(a, tokens, epi, ydt, (hipStream_t)stream));
+    return a;
+}
+
+// the products of codes in the workspace
+qc_status gemm(const Fp8GemmArgs &a, int64_t K, const int32_t *offsets, int64_t experts, const Fp8Plan &plan, qc_epilogue epi,
+               qc_out ydt, void *stream) {
+    if (plan.few.tokens) return device_status(launch_fp8_few(nullptr, QC_F32, K, offsets, (int)experts, a, plan.few, epi, ydt, (hipStream_t)stream));
+    return device_status(launch_fp8_gemm(a, plan.tokens, epi, ydt, (hipStream_t)stream));
+}
+
+// Both launches of a linear, or the one.  Y may lie over X: in two launches X has been read when the products are
+// written; in one launch the blocks that write Y run beside others that still read X.
+qc_status linear(const void *X, qc_dtype xdt, int64_t M, int64_t K, const int32_t *offsets, int64_t experts, const void *packed,
+                 const float *w_scale, int64_t N, const float *bias, qc_epilogue epi, void *Y, qc_out ydt, void *workspace, void *stream) {
+    const size_t x_bytes = (size_t)M * (size_t)K * (xdt == QC_BF16 ? 2 : 4), y_bytes = (size_t)M * (size_t)N * (ydt == QC_OUT_BF16 ? 2 : 4);
+    const Fp8Plan plan = fp8_plan(M, N, K, (int)experts, offsets != nullptr, ydt, !overlap(X, x_bytes, Y, y_bytes));
+    const Fp8GemmArgs a = gemm_args(workspace, M, K, packed, w_scale, N, bias, Y, plan, experts, offsets != nullptr);
+    if (plan.fused) return device_status(launch_fp8_few(X, xdt, K, offsets, (int)experts, a, plan.few, epi, ydt, (hipStream_t)stream));
+    QC_TRY(device_status(launch_fp8_quant(X, xdt, M, K, nullptr, a.x_tiled, a.x_scale, offsets, (int)experts, plan.tokens, a.map, (hipStream_t)stream)));
+    return gemm(a, K, offsets, experts, plan, epi, ydt, stream);
 }
 
 }  // namespace
@@ -124,21 +143,20 @@ extern "C" qc_status qc_qlinear_fp8_gemm(const void *workspace, size_t workspace
     QC_TRY(check_workspace(workspace));
     QC_TRY(check_gemm_supported(M, K, N, 1, ydt));
     if (workspace_bytes < fp8_workspace(M, K).total_bytes) return QC_ERR_WORKSPACE;
-    return gemm(workspace, M, K, packed, w_scale, N, bias, epi, Y, ydt, 1, fp8_gemm_tokens(M, N, K, 1, ydt), false, stream);
+    const Fp8Plan plan = fp8_plan(M, N, K, 1, false, ydt, false);
+    return gemm(gemm_args(const_cast<void *>(workspace), M, K, packed, w_scale, N, bias, Y, plan, 1, false), K, nullptr, 1, plan, epi, ydt, stream);
 }
 
 extern "C" qc_status qc_qlinear_fp8(const void *X, qc_dtype xdt, int64_t M, int64_t K, const void *packed, const float *w_scale,
                                     int64_t N, const float *bias, qc_epilogue epi, void *Y, qc_out ydt, void *workspace,
                                     size_t workspace_bytes, void *stream) {
-    // both halves' checks up front, so that a failed call has no side effect
     QC_TRY(check_activation(X, xdt, M, K));
     QC_TRY(check_weight_side(packed, w_scale, bias, epi, Y, ydt, M, K, N));
     QC_TRY(check_workspace(workspace));
     QC_TRY(check_quant_supported(M, K));
     QC_TRY(check_gemm_supported(M, K, N, 1, ydt));
     if (workspace_bytes < fp8_workspace(M, K).total_bytes) return QC_ERR_WORKSPACE;
-    QC_TRY(qc_qlinear_fp8_quant(X, xdt, M, K, workspace, workspace_bytes, stream));
-    return qc_qlinear_fp8_gemm(workspace, workspace_bytes, M, K, packed, w_scale, N, bias, epi, Y, ydt, stream);
+    return linear(X, xdt, M, K, nullptr, 1, packed, w_scale, N, bias, epi, Y, ydt, workspace, stream);
 }
 
 extern "C" qc_status qc_qlinear_fp8_grouped(const void *X, qc_dtype xdt, int64_t M, int64_t K, const int32_t *expert_offsets,
@@ -152,11 +170,18 @@ extern "C" qc_status qc_qlinear_fp8_grouped(const void *X, qc_dtype xdt, int64_t
     if (experts > QC_MAX_EXPERTS) return QC_ERR_UNSUPPORTED;
     QC_TRY(check_quant_supported(M, K));
     QC_TRY(check_gemm_supported(M, K, N, experts, ydt));
-    const Fp8Workspace ws = fp8_workspace(M, K);
-    if (workspace_bytes < ws.total_bytes) return QC_ERR_WORKSPACE;
-    uint8_t *const base = (uint8_t *)workspace;
-    const int tokens = fp8_gemm_tokens(M, N, K, (int)experts, ydt);
-    QC_TRY(device_status(launch_fp8_quant(X, xdt, M, K, nullptr, base + ws.codes_offset, (float *)base, expert_offsets, (int)experts,
-                                          tokens, (Fp8Tile *)(base + ws.map_offset), (hipStream_t)stream)));
-    return gemm(workspace, M, K, packed, w_scale, N, bias, epi, Y, ydt, (int)experts, tokens, true, stream);
+    if (workspace_bytes < fp8_workspace(M, K).total_bytes) return QC_ERR_WORKSPACE;
+    return linear(X, xdt, M, K, expert_offsets, experts, packed, w_scale, N, bias, epi, Y, ydt, workspace, stream);
+}
+
+extern "C" int qc_debug_linear_plan_fp8(int64_t M, int64_t K, int64_t N, int64_t experts, qc_out ydt, int32_t *plan) {
+    if (M < 1 || K < 1 || N < 1 || experts < 0 || !plan || (ydt != QC_OUT_F32 && ydt != QC_OUT_BF16)) return -1;
+    const int64_t matrices = experts ? experts : 1;
+    if (check_quant_supported(M, K) != QC_OK || check_gemm_supported(M, K, N, matrices, ydt) != QC_OK) return -1;
+    const Fp8Plan p = fp8_plan(M, N, K, (int)matrices, experts != 0, ydt, true);
+    plan[0] = p.few.tokens ? kGemmSmall : kGemmRing;
+    plan[1] = p.tokens;
+    plan[2] = p.few.tokens ? kFragRows * p.few.frags : kTileN;
+    plan[3] = p.fused;
+    return 0;
 }

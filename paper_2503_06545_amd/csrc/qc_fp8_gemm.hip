@@ -4,59 +4,12 @@
 //
 // One v_mfma_f32_16x16x128_f8f6f4 covers a block, so P_b comes out of the matrix unit with nothing to add it to, and the
 // scales are one fma per output and block on the vector unit, half as many issue cycles as the matrix instruction's.
-#include <type_traits>
-
-#include "qc_device.h"
-#include "qc_fp8.h"
+#include "qc_fp8_device.h"
 
 namespace qc {
 namespace {
 
-typedef int v4i __attribute__((ext_vector_type(4)));
-typedef int v8i __attribute__((ext_vector_type(8)));
-typedef float f4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
 constexpr int kThreads = 256;
-
-// One operand of 16 rows x 128 k as the matrix unit takes it.  The instructions for e4m3 operands line up eight products with
-// the largest of them before they add, and drop what is then too low: the sum of a block comes out 1.5e-5 off (2-norm,
-// normal values), where the instruction for bf16 operands is 1e-8 off.  That is enough for outputs that are rounded to bf16
-// (2^-9 each), not for binary32 ones.  EXACT widens the codes to bf16, exactly, and takes four instructions of 32 k instead
-// of one of 128 (registers only, random operands, TFLOP/s: 4390 and 2260).
-template <bool EXACT>
-struct Operand;
-template <>
-struct Operand<false> {
-    v8i v;
-    __device__ Operand() {}
-    __device__ Operand(v4i lo, v4i hi) : v(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)) {}
-};
-template <>
-struct Operand<true> {
-    bf16x8 v[4];
-    __device__ Operand() {}
-    __device__ Operand(v4i lo, v4i hi) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int d0 = j < 2 ? lo[2 * j] : hi[2 * j - 4], d1 = j < 2 ? lo[2 * j + 1] : hi[2 * j - 3];
-            const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(d0, 1.0f, false), p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(d0, 1.0f, true);
-            const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(d1, 1.0f, false), p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(d1, 1.0f, true);
-            v[j] = bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
-        }
-    }
-};
-
-__device__ inline f4 product(const Operand<false> &a, const Operand<false> &b) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, f4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
-}
-__device__ inline f4 product(const Operand<true> &a, const Operand<true> &b) {
-    f4 c = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[j], b.v[j], c, 0, 0, 0);
-    return c;
-}
 
 template <int EPI>
 __device__ inline float activation(float y) {
@@ -65,11 +18,6 @@ __device__ inline float activation(float y) {
     return y;
 }
 
-// which rows a block's tile has and whose weights it takes
-struct Where {
-    int64_t row0;
-    int rows, expert;
-};
 __device__ inline Where tile_of(const Fp8GemmArgs &a, int v, int tokens) {
     if (a.map) {
         const Fp8Tile t = a.map[v];
@@ -338,10 +286,70 @@ hipError_t launch_tiles(const Fp8GemmArgs &a, qc_epilogue epi, hipStream_t strea
 
 }  // namespace
 
-int fp8_gemm_tokens(int64_t M, int64_t N, int64_t K, int experts, qc_out ydt) { return ydt == QC_OUT_F32 ? 128 : 192; }
+constexpr int kCus = 256;
+
+// What a CU takes for a step of `per_cu` of the ring kernel's tiles of 64 h tokens, in hundredths of a microsecond, read off
+// linears of 300 to 20000 tokens at every height.  A tile that a CU has to itself waits out its own loads, which a lower one has
+// fewer of; from two or three on the products count, and for binary32 outputs their widening.  (us at 192 / 128 / 64 tokens:
+// 300 x 4608 x 1152 31.3 25.2 20.2, 2400 x 4608 x 1152 37.7 31.6 32.3, 5000 x 4608 x 1152 46.0 49.2 51.3, 5000 x 1152 x 4608 41.5 39.8
+// 47.0, 20000 x 1152 x 4608 126 130 162; binary32, 128 / 64: 300 x 4608 x 1152 46.0 34.7, 4099 x 1000 x 1301 31.3 28.8, 10000 x
+// 1152 x 4608 132 144.)
+static double step_cost(int h, double per_cu, bool exact, bool lengthy) {
+    if (exact) return h == 1 ? (per_cu <= 1 ? 85 : per_cu <= 2 ? 140 : 68 * per_cu) : per_cu <= 1 ? 115 : per_cu <= 2 ? 210 : 120 * per_cu;
+    if (h == 1) return per_cu <= 1 ? 45 : per_cu <= 2 ? 69 : (lengthy ? 44 : 37) * per_cu;
+    if (h == 2) return per_cu <= 1 ? 60 : per_cu <= 2 ? 110 : 60 * per_cu;
+    return per_cu <= 1 ? 85 : 88 * per_cu;
+}
+
+static int ring_tokens(int64_t M, int64_t N, int experts, bool grouped, bool exact, bool lengthy) {
+    const int64_t n_tiles = round_up(N, kTileN) / kTileN;
+    int best = 0;
+    double least = 0;
+    for (int h = exact ? 2 : 3; h >= 1; --h) {
+        double per_cu;
+        if (grouped) {   // half a tile more than its rows fill for each expert that has any
+            const double live = (double)(experts < M ? experts : M), each = (double)M / live / (64 * h) + 0.5;
+            per_cu = live * (each > 1 ? each : 1) * (double)n_tiles / kCus;
+        } else {
+            const int64_t tiles = (M + 64 * h - 1) / (64 * h) * n_tiles;
+            per_cu = tiles <= 4 * kCus ? (double)((tiles + kCus - 1) / kCus) : (double)tiles / kCus;
+        }
+        const double cost = step_cost(h, per_cu, exact, lengthy);
+        if (best == 0 || cost < least) { best = h; least = cost; }
+    }
+    return 64 * best;
+}
+
+// The few-token kernel, from X in one launch while its tiles of 16 tokens x 64 channels are at most two to a CU, with fewer
+// channels where that gives at most one (us at 16, 32 and 64 channels: 1 x 1152 x 6912 6.7 4.6 5.0, 1 x 4608 x 1152 7.6 8.0 8.8, 64 x 1152
+// x 1152 7.3 4.9 5.6, 162 rows of 52 experts, 1152 x 44, 8.5 5.8 6.2; the ring 12.5 29.6 12.6 10.8).  A long reduction casts more in
+// each block than more than 64 tokens are worth, a very long one at all (137 rows of 3 experts, 3909 x 1187, 18.1, from codes 13.6; 47 x
+// 6813 x 89 20.8 14.4).  From codes with tiles of 32 x 64 while these are at most one to a CU (300 x 4608 x 1152 13.5, ring of 64
+// tokens 20.2; binary32 17.0 34.7), with a long reduction two for binary32 outputs (600 x 4608 x 1152 28 36).
+Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, int experts, bool grouped, qc_out ydt, bool may_fuse) {
+    Fp8Plan p{};
+    const bool exact = ydt == QC_OUT_F32, lengthy = fp8_blocks(K) >= 18;
+    const int64_t most = 2 * kCus * 8 * kTileN;   // beyond this the tile counts below need not be made
+    if (M <= most && N <= most) {
+        auto tiles = [&](int tokens, int frags) {
+            const int64_t m = grouped ? fp8_tiles_most(M, experts, tokens) : (M + tokens - 1) / tokens;
+            return m * (round_up(N, kTileN) / kTileN) * (8 / frags);   // a tile's channels lie eight apart: any N has all of a group's
+        };
+        if (may_fuse && tiles(16, 4) <= 2 * kCus && M <= (lengthy ? 64 : 512) && fp8_blocks(K) <= 36) {
+            p.fused = true;
+            p.few = {16, tiles(16, 1) <= kCus / 2 ? 1 : tiles(16, 2) <= kCus ? 2 : 4};
+        } else if (tiles(32, 4) <= (exact && lengthy ? 2 : 1) * kCus) {
+            p.few = {32, 4};
+        }
+    }
+    p.tokens = p.few.tokens ? p.few.tokens : ring_tokens(M, N, experts, grouped, exact, lengthy);
+    return p;
+}
 
 hipError_t launch_fp8_gemm(const Fp8GemmArgs &args, int tokens, qc_epilogue epi, qc_out ydt, hipStream_t stream) {
-    if (ydt == QC_OUT_F32) return launch_tiles<2, QC_OUT_F32>(args, epi, stream);
+    if (ydt == QC_OUT_F32) return tokens == 64 ? launch_tiles<1, QC_OUT_F32>(args, epi, stream) : launch_tiles<2, QC_OUT_F32>(args, epi, stream);
+    if (tokens == 64) return launch_tiles<1, QC_OUT_BF16>(args, epi, stream);
+    if (tokens == 128) return launch_tiles<2, QC_OUT_BF16>(args, epi, stream);
     return launch_tiles<3, QC_OUT_BF16>(args, epi, stream);
 }
 

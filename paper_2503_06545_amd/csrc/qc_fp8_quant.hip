@@ -7,8 +7,7 @@
 // row (see Group in qc_device.h), so a block's maximum is three DPP steps away and nothing has to wait for the rest of the
 // row.  The quotient is computed as in qc_quant.hip, from one division per block; values whose quotient is too small for
 // that to be exact round to a zero code either way.
-#include "qc_device.h"
-#include "qc_fp8.h"
+#include "qc_fp8_device.h"
 
 namespace qc {
 namespace {
@@ -17,36 +16,11 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kRowsPerWave = 8;   // eight lanes each
 
 // eight lanes' share of columns col0 .. col0 + 127 of a row of K at any alignment, zeros past its end
-template <typename XT, bool NT>
+template <typename XT>
 __device__ inline void load_block(Group<XT> &g, const XT *xrow, int64_t col0, int64_t K, int sub) {
     constexpr int E = 16 / (int)sizeof(XT), P = sizeof(g.v) / sizeof(g.v[0]);
 #pragma unroll
-    for (int j = 0; j < P; ++j) {
-        const int64_t col = col0 + 8 * E * j + E * sub;
-        const int64_t past = col + E - K;   // elements of the piece past the row's end
-        if (past <= 0) {
-            const u32x4_any t = *reinterpret_cast<const u32x4_any *>(xrow + col);
-            g.v[j] = make_uint4(t.x, t.y, t.z, t.w);
-        } else if (past >= E) {
-            g.v[j] = make_uint4(0, 0, 0, 0);
-        } else if (K >= E) {   // loaded so that it ends with the row, and moved down
-            const u32x4_any t = *reinterpret_cast<const u32x4_any *>(xrow + K - E);
-            g.v[j] = move_down(make_uint4(t.x, t.y, t.z, t.w), (int)past * (int)(sizeof(XT) / 2));
-        } else {               // a row of less than 16 B
-            uint32_t w[4] = {0, 0, 0, 0};
-            for (int e = 0; e < (int)(E - past); ++e) {
-                if constexpr (sizeof(XT) == 4) w[e] = __float_as_uint(xrow[col + e]);
-                else w[e / 2] |= (uint32_t)xrow[col + e] << (16 * (e % 2));
-            }
-            g.v[j] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-    }
-}
-
-// four quotients -> four e4m3 codes in a dword, element 0 lowest
-__device__ inline uint32_t e4m3x4(float q0, float q1, float q2, float q3) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(q0, q1, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q2, q3, w, true);
+    for (int j = 0; j < P; ++j) g.v[j] = load_piece(xrow, col0 + 8 * E * j + E * sub, K);
 }
 
 struct QuantArgs {
@@ -133,13 +107,13 @@ __global__ __launch_bounds__(kThreads) void fp8_quant_kernel(QuantArgs a) {
     const int chunk = blockIdx.x % (uint32_t)a.chunks;
     const int64_t row0 = (row_block * kWaves + wave) * kRowsPerWave, row = row0 + lane / 8;
     if (row >= a.M) return;
-    if (a.map && (row < a.offsets[0] || row >= a.offsets[a.experts])) return;   // of no group
+    if (a.offsets && (row < a.offsets[0] || row >= a.offsets[a.experts])) return;   // of no group
     const XT *const xrow = reinterpret_cast<const XT *>(a.X) + row * a.K;
     const int b0 = chunk * GROUPS;
 
     Group<XT> g[GROUPS];
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) load_block<XT, false>(g[i], xrow, (int64_t)(b0 + i) * kFp8Block, a.K, sub);
+    for (int i = 0; i < GROUPS; ++i) load_block(g[i], xrow, (int64_t)(b0 + i) * kFp8Block, a.K, sub);
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
         if (b0 + i >= a.KB) break;
@@ -236,14 +210,14 @@ hipError_t launch_fp8_quant(const void *X, qc_dtype xdt, int64_t M, int64_t K, u
     constexpr int G = 3;
     a.chunks = (a.KB + G - 1) / G;
     a.quant_blocks = (int)((M + kWaves * kRowsPerWave - 1) / (kWaves * kRowsPerWave) * a.chunks);
-    if (offsets) {
-        a.offsets = offsets;
+    a.offsets = offsets;
+    a.experts = experts;
+    if (map) {
         a.map = map;
-        a.experts = experts;
         a.tokens = tokens;
         a.map_entries = (int)fp8_tiles_most(M, experts, tokens);
     }
-    const dim3 grid((unsigned)(a.quant_blocks + (offsets ? 1 : 0))), block(kThreads);
+    const dim3 grid((unsigned)(a.quant_blocks + (map ? 1 : 0))), block(kThreads);
     if (xdt == QC_BF16) fp8_quant_kernel<uint16_t, G><<<grid, block, 0, stream>>>(a);
     else fp8_quant_kernel<float, G><<<grid, block, 0, stream>>>(a);
     return hipGetLastError();

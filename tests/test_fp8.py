@@ -141,3 +141,24 @@ def test_bf16_inputs_are_widened_before_the_quantizer():
     bits = synth.to_bf16_bits(x)
     for got, want in zip(oracle.quant_act_fp8(bits), oracle.quant_act_fp8(oracle.widen_f32(bits))):
         assert np.array_equal(got, want)
+
+
+def test_plans():
+    """Few tokens go out in one launch, a long reduction of a few hundred through the same kernel from codes, many through the
+    ring, on lower tiles the fewer there are; what is refused has no plan."""
+    plan = qc.linear_plan_fp8
+    assert plan(1, 1152, 6912) == {"kernel": "few", "tokens": 16, "channels": 32, "fused": True}
+    assert plan(1, 4608, 1152)["channels"] == 16 and plan(130, 1152, 1152)["channels"] == 64
+    assert plan(300, 4608, 1152) == {"kernel": "few", "tokens": 32, "channels": 64, "fused": False}
+    assert plan(600, 4608, 1152, "f32")["kernel"] == "few" and plan(600, 4608, 1152)["kernel"] == "ring"
+    assert plan(131072, 1152, 4608) == {"kernel": "ring", "tokens": 192, "channels": 128, "fused": False}
+    assert plan(131072, 1152, 4608, "f32")["tokens"] == 128 and plan(1200, 1152, 1152)["tokens"] == 64
+    assert plan(8, 4608, 1152, experts=32)["fused"] and plan(200, 1152, 4608, experts=32)["tokens"] == 64
+    assert plan(16000, 1152, 4608, experts=64)["tokens"] == 128
+    for bad in ((0, 8, 8), (8, qc.QC_MAX_K + 1, 8), (8, 8, qc.QC_MAX_N + 1)):
+        with pytest.raises(qc.QcError):
+            plan(*bad)
+    with pytest.raises(qc.QcError):
+        plan(8, 8, 8, experts=qc.QC_MAX_EXPERTS + 1)
+    with pytest.raises(qc.QcError):
+        plan(8, 8, 8, "i32")

@@ -173,6 +173,35 @@ def test_what_the_e4m3_instruction_keeps():
             assert (y[2:34] == 2.0 ** e).all() and (y[34:] == 0).all() and (y[:2] == 0).all(), (out, e)
 
 
+def which(M, K, N, out, experts=0):
+    p = qc.linear_plan_fp8(M, K, N, out, experts)
+    return p["kernel"], p["tokens"], p["channels"], p["fused"]
+
+
+KERNELS = [("few", 16, 16, True), ("few", 16, 32, True), ("few", 16, 64, True), ("few", 32, 64, False), ("ring", 64, 128, False),
+           ("ring", 128, 128, False)]
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N,out,kernel", [
+    (5, 700, 700, "f32", 0), (5, 700, 700, "bf16", 0), (20, 1153, 2311, "f32", 1), (20, 1153, 2311, "bf16", 1), (70, 513, 4609, "f32", 2), (70, 513, 4609, "bf16", 2),
+    (150, 5001, 700, "f32", 3), (150, 5001, 700, "bf16", 3), (550, 260, 2200, "f32", 4), (550, 260, 2200, "bf16", 4),
+    (16500, 130, 1301, "f32", 5), (1500, 384, 5100, "bf16", 5), (20500, 257, 1301, "bf16", 6)])
+def test_every_kernel_at_ragged_sizes(M, K, N, out, kernel, x):
+    assert which(M, K, N, out) == (KERNELS + [("ring", 192, 128, False)])[kernel]
+    run_linear(np.random.default_rng(kernel), M, K, N, x, out, bias=kernel % 2 == 0)
+
+
+@pytest.mark.parametrize("M,K,N,E,out,kernel", [(9, 200, 1000, 4, "f32", 1), (40, 300, 2000, 5, "bf16", 2), (100, 5001, 130, 3, "bf16", 3), (100, 5001, 130, 3, "f32", 3),
+                                                (600, 300, 1300, 6, "bf16", 4), (600, 300, 1300, 6, "f32", 4), (16000, 130, 1000, 64, "bf16", 5),
+                                                (20000, 130, 701, 2, "f32", 5), (3300, 257, 3301, 2, "bf16", 6)])
+def test_every_kernel_grouped(M, K, N, E, out, kernel):
+    assert which(M, K, N, out, E) == (KERNELS + [("ring", 192, 128, False)])[kernel]
+    rng = np.random.default_rng(kernel + M)
+    cut = sorted(int(v) for v in rng.integers(0, M, size=E))
+    run_grouped(rng, M, K, N, [0, *cut], "bf16", out)
+
+
 # the sizes of real layers, sampled: the rows of a small block repeated, every row against the block's
 @pytest.mark.parametrize("M,K,N,out,epi", [(16384, 1152, 3456, "bf16", "none"), (20000, 4608, 1152, "f32", "none"), (9000, 1152, 4608, "bf16", "gelu_tanh"),
                                            (4099, 1000, 1301, "f32", "gelu_erf"), (2500, 9216, 640, "bf16", "none"), (700000, 128, 3200, "bf16", "none")])
