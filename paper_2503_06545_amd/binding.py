@@ -851,6 +851,8 @@ def qlinear_fp8_workspace_t(M: int, K: int, N: int, device="cuda"):
 def _fp8_linear_operands(X, pw, bias, out, workspace, Y, bias_shape):
     torch = _torch()
     _fp8_activation(X, pw.K)
+    _fp8_operand(pw.blob, "pw.blob", (torch.uint8,), (None,))
+    _fp8_operand(pw.scale, "pw.scale", (torch.float32,), (pw.experts, -(-pw.N // QC_FP8_BLOCK), -(-pw.K // QC_FP8_BLOCK)))
     ydtype = {"f32": torch.float32, "bf16": torch.bfloat16}[out]
     if bias is not None:
         _fp8_operand(bias, "bias", (torch.float32,), bias_shape)
@@ -892,13 +894,14 @@ def qlinear_fp8_grouped_t(X, pw: PackedWeightFp8, expert_offsets, bias=None, epi
 # ---- the per-step helpers as native functions ----------------------------------------------------
 
 _PER_STEP = ("qlinear_t", "qlinear_asym_t", "qlinear_tensor_t", "latent_delta_t", "layer_similarity_t",
-             "frame_gradient_norm_t", "cumulative_variation_t")
+             "frame_gradient_norm_t", "cumulative_variation_t", "quant_act_fp8_t", "qlinear_fp8_t", "qlinear_fp8_grouped_t")
 
 
 def _entries():
     """The addresses of the C entries behind _PER_STEP, in that order, and of the rotated linear."""
     names = ("qc_qlinear_act_bits", "qc_qlinear_asym", "qc_qlinear_tensor", "qc_latent_delta", "qc_layer_similarity",
-             "qc_frame_gradient_norm", "qc_cumulative_variation", "qc_qlinear_rot")
+             "qc_frame_gradient_norm", "qc_cumulative_variation", "qc_quant_act_fp8", "qc_qlinear_fp8", "qc_qlinear_fp8_grouped",
+             "qc_qlinear_rot")
     return tuple(ctypes.cast(getattr(lib(), n), ctypes.c_void_p).value for n in names)
 
 

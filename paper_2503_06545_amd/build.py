@@ -79,7 +79,7 @@ def _compile_torch(_=None) -> str:
     includes = [os.path.join(ROOT, "include"), os.path.join(base, "include"), "/opt/rocm/include", sysconfig.get_paths()["include"],
                 os.path.join(base, "include", "torch", "csrc", "api", "include")]
     subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
-                    *("-I" + i for i in includes), TORCH_SRC, "-o", TORCH_LIB, "-L" + lib, "-ltorch_python", "-lc10",
+                    *("-I" + i for i in includes), TORCH_SRC, "-o", TORCH_LIB, "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10",
                     "-lc10_hip", "-Wl,-rpath," + lib], check=True)
     return TORCH_LIB
 

@@ -10,7 +10,9 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -18,7 +20,7 @@
 
 namespace {
 
-enum Helper { kLinear, kAsym, kTensor, kDelta, kSimilarity, kGradient, kVariation, kHelpers };
+enum Helper { kLinear, kAsym, kTensor, kDelta, kSimilarity, kGradient, kVariation, kQuantFp8, kLinearFp8, kGroupedFp8, kHelpers };
 constexpr int kArgsMost = 9;
 const char *const kNames[kHelpers][kArgsMost] = {
     {"X", "pw", "bias", "epi", "out", "workspace", "Y", "act_bits", "rot_block"},
@@ -28,9 +30,12 @@ const char *const kNames[kHelpers][kArgsMost] = {
     {"a", "b", "workspace", "out4"},
     {"m", "workspace", "out2"},
     {"cur", "prevs", "workspace", "out"},
+    {"X", "qx", "x_scale"},
+    {"X", "pw", "bias", "epi", "out", "workspace", "Y"},
+    {"X", "pw", "expert_offsets", "bias", "epi", "out", "workspace", "Y"},
 };
 PyObject *names[kHelpers][kArgsMost];   // interned, made once, kept
-PyObject *attr_blob, *attr_scale, *attr_N, *attr_K, *attr_bits;
+PyObject *attr_blob, *attr_scale, *attr_N, *attr_K, *attr_bits, *attr_experts;
 
 // what one import of the module holds; the C entries are asked for on the first call
 struct State {
@@ -325,6 +330,115 @@ PyObject *cumulative_variation_t(PyObject *m, PyObject *const *args, Py_ssize_t 
     });
 }
 
+// ---- 8-bit floating point with a scale for every block of 128 ----
+
+// a dense tensor of this type and shape on the device that launches go to
+bool operand(const at::Tensor &t, at::ScalarType type, at::IntArrayRef shape, int device) {
+    return t.scalar_type() == type && t.sizes() == shape && t.is_contiguous() && t.is_cuda() && t.get_device() == device;
+}
+bool activation_fp8(const at::Tensor &X, qc_dtype &xdt, int device) {
+    return data_type(X, xdt) && X.dim() == 2 && X.is_contiguous() && X.is_cuda() && X.get_device() == device;
+}
+struct Reference {   // one of its own
+    PyObject *object = nullptr;
+    ~Reference() { Py_XDECREF(object); }
+};
+int64_t blocks_of(int64_t n) { return (n + QC_FP8_BLOCK - 1) / QC_FP8_BLOCK; }
+
+PyObject *quant_act_fp8_t(PyObject *m, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
+    return helper<kQuantFp8, 3>(m, args, n, kw, [](const Call &c, PyObject *&r) {
+        const at::Tensor *const X = tensor(c.a[0]);
+        const int device = c10::hip::current_device();
+        qc_dtype xdt;
+        if (!X || !activation_fp8(*X, xdt, device)) return false;
+        const int64_t M = X->size(0), K = X->size(1);
+        Reference outputs[2];
+        for (int i = 0; i < 2; ++i) {
+            const auto type = i ? at::kFloat : at::kFloat8_e4m3fn;
+            const int64_t shape[2] = {M, i ? blocks_of(K) : K};
+            PyObject *const given = c.a[1 + i];
+            if (given && given != Py_None) {
+                const at::Tensor *const t = tensor(given);
+                if (!t || !operand(*t, type, shape, device)) return false;
+                Py_INCREF(given);
+                outputs[i].object = given;
+            } else if (!(outputs[i].object = THPVariable_Wrap(at::empty(shape, X->options().dtype(type).requires_grad(false))))) {
+                return false;
+            }
+        }
+        uint8_t *const codes = static_cast<uint8_t *>(THPVariable_Unpack(outputs[0].object).data_ptr());
+        float *const scales = static_cast<float *>(THPVariable_Unpack(outputs[1].object).data_ptr());
+        const void *const x = X->data_ptr();
+        void *const stream = current_stream();
+        int status;
+        Py_BEGIN_ALLOW_THREADS
+        status = reinterpret_cast<decltype(&qc_quant_act_fp8)>(c.s->entry[kQuantFp8])(x, xdt, M, K, codes, scales, stream);
+        Py_END_ALLOW_THREADS
+        Reference pair{PyTuple_Pack(2, outputs[0].object, outputs[1].object)};
+        if (pair.object) r = c.finish(status, "qc_quant_act_fp8", pair.object);
+        return true;
+    });
+}
+
+// the linear and the grouped one; at: where their common arguments from `bias` on begin
+bool linear_fp8(const Call &c, int at, PyObject *offsets_object, PyObject *&result) {
+    const at::Tensor *const X = tensor(c.a[0]), *const ws = tensor(c.a[at + 3]), *const Y = tensor(c.a[at + 4]);
+    PyObject *const bias_object = c.a[at] ? c.a[at] : Py_None;
+    const at::Tensor *const bias = bias_object == Py_None ? nullptr : tensor(bias_object);
+    const bool grouped = c.which == kGroupedFp8;
+    const at::Tensor *const offsets = grouped ? tensor(offsets_object) : nullptr;
+    PyObject *const pw = c.a[1];
+    if (!X || !ws || !Y || !pw || (bias_object != Py_None && !bias) || (grouped && !offsets)) return false;
+    int epi, out;
+    if (!choice(c.a[at + 1], kEpilogues, 3, epi) || !choice(c.a[at + 2], kOuts, 2, out)) return false;
+    long experts, N, K;
+    if (!Weight::number(pw, attr_experts, experts) || !Weight::number(pw, attr_N, N) || !Weight::number(pw, attr_K, K)) return false;
+    const int device = c10::hip::current_device();
+    const void *blob;
+    const float *scale;
+    {
+        PyObject *const b = PyObject_GetAttr(pw, attr_blob), *const s = b ? PyObject_GetAttr(pw, attr_scale) : nullptr;
+        const at::Tensor *const tb = tensor(b), *const ts = tensor(s);
+        const bool ok = tb && ts && operand(*tb, at::kByte, {tb->numel()}, device) &&
+                        operand(*ts, at::kFloat, {experts, blocks_of(N), blocks_of(K)}, device);
+        blob = ok ? tb->data_ptr() : nullptr;
+        scale = ok ? static_cast<const float *>(ts->data_ptr()) : nullptr;
+        Py_XDECREF(b);
+        Py_XDECREF(s);
+        if (!ok) return false;
+    }
+    qc_dtype xdt;
+    if (!activation_fp8(*X, xdt, device) || X->size(1) != K) return false;
+    const int64_t M = X->size(0);
+    if (!operand(*Y, out == 0 ? at::kBFloat16 : at::kFloat, {M, N}, device) || !operand(*ws, at::kByte, {ws->numel()}, device)) return false;
+    if (grouped ? !operand(*offsets, at::kInt, {experts + 1}, device) : experts != 1) return false;
+    if (bias && !(grouped ? operand(*bias, at::kFloat, {experts, N}, device) : operand(*bias, at::kFloat, {N}, device))) return false;
+    const void *const x = X->data_ptr();
+    const int32_t *const off = grouped ? static_cast<const int32_t *>(offsets->data_ptr()) : nullptr;
+    const float *const b = bias ? static_cast<const float *>(bias->data_ptr()) : nullptr;
+    void *const y = Y->data_ptr(), *const space = ws->data_ptr(), *const stream = current_stream();
+    const size_t bytes = (size_t)ws->numel();
+    const qc_epilogue e = kEpilogueOf[epi];
+    const qc_out o = kOutOf[out];
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    if (grouped)
+        status = reinterpret_cast<decltype(&qc_qlinear_fp8_grouped)>(c.s->entry[kGroupedFp8])(x, xdt, M, K, off, experts, blob, scale, N, b, e, y, o,
+                                                                                             space, bytes, stream);
+    else
+        status = reinterpret_cast<decltype(&qc_qlinear_fp8)>(c.s->entry[kLinearFp8])(x, xdt, M, K, blob, scale, N, b, e, y, o, space, bytes, stream);
+    Py_END_ALLOW_THREADS
+    result = c.finish(status, grouped ? "qc_qlinear_fp8_grouped" : "qc_qlinear_fp8", c.a[at + 4]);
+    return true;
+}
+
+PyObject *qlinear_fp8_t(PyObject *m, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
+    return helper<kLinearFp8, 7>(m, args, n, kw, [](const Call &c, PyObject *&r) { return linear_fp8(c, 2, nullptr, r); });
+}
+PyObject *qlinear_fp8_grouped_t(PyObject *m, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
+    return helper<kGroupedFp8, 8>(m, args, n, kw, [](const Call &c, PyObject *&r) { return linear_fp8(c, 3, c.a[2], r); });
+}
+
 // setup(resolve, check, (the Python helpers, in the order of Helper)).  resolve() -> the addresses of the C entries, in
 // that order and qc_qlinear_rot last; check(status, where) raises.
 PyObject *setup(PyObject *module, PyObject *args) {
@@ -360,6 +474,13 @@ PyMethodDef methods[] = {
               "m: [frames, ...] float32 or bfloat16, contiguous -> device float [2]."),
     QC_METHOD(cumulative_variation_t, "($module, cur, prevs, workspace=None, out=None)",
               "cur float32 [n], prevs a list of float32 tensors of the same size -> device float\n[len(prevs) + 1]."),
+    QC_METHOD(quant_act_fp8_t, "($module, X, qx=None, x_scale=None)",
+              "X [M, K] -> codes float8_e4m3fn [M, K], scales float32 [M, ceil(K / 128)]; into qx and x_scale if given."),
+    QC_METHOD(qlinear_fp8_t, "($module, X, pw, bias=None, epi='none', out='bf16', workspace=None, Y=None)",
+              "X [M, K] float32 or bfloat16, pw of one matrix, bias float32 [N] -> Y [M, N]."),
+    QC_METHOD(qlinear_fp8_grouped_t, "($module, X, pw, expert_offsets, bias=None, epi='none', out='bf16', workspace=None, Y=None)",
+              "X [M, K], its rows sorted by expert; expert_offsets int32 [experts + 1] on the GPU; bias float32 [experts, N]\n"
+              "-> Y [M, N], in which rows of no group stay as they were."),
     {"setup", setup, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
@@ -386,9 +507,9 @@ int execute(PyObject *) {
     for (int w = 0; w < kHelpers; ++w)
         for (int i = 0; i < kArgsMost && kNames[w][i]; ++i)
             if (!names[w][i] && !(names[w][i] = PyUnicode_InternFromString(kNames[w][i]))) return -1;
-    PyObject **const attrs[] = {&attr_blob, &attr_scale, &attr_N, &attr_K, &attr_bits};
-    const char *const texts[] = {"blob", "scale", "N", "K", "bits"};
-    for (int i = 0; i < 5; ++i)
+    PyObject **const attrs[] = {&attr_blob, &attr_scale, &attr_N, &attr_K, &attr_bits, &attr_experts};
+    const char *const texts[] = {"blob", "scale", "N", "K", "bits", "experts"};
+    for (int i = 0; i < 6; ++i)
         if (!*attrs[i] && !(*attrs[i] = PyUnicode_InternFromString(texts[i]))) return -1;
     return 0;
 }

@@ -458,3 +458,46 @@ def test_helpers_refuse_tensors_of_other_kinds_on_the_gpu():
         qc.qlinear_fp8_t(X, pw, workspace=torch.zeros(256, dtype=torch.uint8, device="cuda"))
     with pytest.raises(qc.QcError):
         qc.qlinear_fp8_t(torch.zeros(0, 16, device="cuda"), pw)
+
+
+def test_native_helpers_are_the_python_ones():
+    """The same bits, tensors and errors, in any form of the call."""
+    qc._use_native_helpers()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    X = torch.randn(40, 300, generator=g, device="cuda").bfloat16()
+    W = torch.randn(3, 70, 300, generator=g, device="cuda")
+    pw, one = qc.pack_weight_fp8_t(W), qc.pack_weight_fp8_t(W[0].contiguous())
+    off, bias = torch.tensor([0, 11, 11, 40], dtype=torch.int32, device="cuda"), torch.randn(3, 70, generator=g, device="cuda")
+    ws = qc.qlinear_fp8_workspace_t(40, 300, 70)
+
+    def Y(dtype=torch.bfloat16):
+        return torch.zeros(40, 70, dtype=dtype, device="cuda")
+
+    calls = [("quant_act_fp8_t", (X,), dict), ("quant_act_fp8_t", (X.float(),), lambda: dict(x_scale=torch.empty(40, 3, device="cuda"))),
+             ("quant_act_fp8_t", (X, torch.empty(40, 300, dtype=torch.float8_e4m3fn, device="cuda")), dict),
+             ("quant_act_fp8_t", (X, torch.empty(40, 299, dtype=torch.float8_e4m3fn, device="cuda")), dict), ("quant_act_fp8_t", (X.t(),), dict),
+             ("quant_act_fp8_t", (X.half(),), dict), ("quant_act_fp8_t", (X[:0],), dict), ("quant_act_fp8_t", (X.cpu(),), dict),
+             ("qlinear_fp8_t", (X, one), lambda: dict(workspace=ws, Y=Y(), bias=bias[0])), ("qlinear_fp8_t", (X, one), dict),
+             ("qlinear_fp8_t", (X, one, bias[1], "gelu_erf", "f32", ws), lambda: dict(Y=Y(torch.float32))),
+             ("qlinear_fp8_t", (X, one), lambda: dict(workspace=ws, Y=Y(torch.float32))), ("qlinear_fp8_t", (X, one), lambda: dict(workspace=ws[:64], Y=Y())),
+             ("qlinear_fp8_t", (X, pw), lambda: dict(workspace=ws, Y=Y())), ("qlinear_fp8_t", (X, one), lambda: dict(workspace=ws, Y=Y(), bias=bias)),
+             ("qlinear_fp8_t", (X, one), lambda: dict(workspace=ws, Y=Y(), epi="relu")), ("qlinear_fp8_t", (X, one), lambda: dict(workspace=ws, Y=Y(), out="i32")),
+             ("qlinear_fp8_t", (X[:, :299], one), lambda: dict(workspace=ws, Y=Y())), ("qlinear_fp8_t", (X, None), lambda: dict(workspace=ws, Y=Y())),
+             ("qlinear_fp8_grouped_t", (X, pw, off), lambda: dict(workspace=ws, Y=Y(), bias=bias, epi="gelu_tanh")),
+             ("qlinear_fp8_grouped_t", (X, pw, off), lambda: dict(workspace=ws)), ("qlinear_fp8_grouped_t", (X, one, off[:2]), lambda: dict(workspace=ws, Y=Y())),
+             ("qlinear_fp8_grouped_t", (X, pw, off.long()), lambda: dict(workspace=ws, Y=Y())), ("qlinear_fp8_grouped_t", (X, pw, off[1:]), lambda: dict(workspace=ws, Y=Y())),
+             ("qlinear_fp8_grouped_t", (X, pw, off), lambda: dict(workspace=ws, Y=Y(), bias=bias[0]))]
+
+    def outcome(f, args, kwargs):
+        try:
+            r = f(*args, **kwargs)
+        except Exception as e:   # the type and the text are what is compared
+            return type(e), str(e)
+        return [t.clone() for t in (r if isinstance(r, tuple) else (r,))]
+
+    for name, args, options in calls:
+        want, got = outcome(qc._python_helpers[name], args, options()), outcome(getattr(qc, name), args, options())
+        if isinstance(want, tuple):
+            assert got == want, (name, got, want)
+        else:
+            assert isinstance(got, list) and all(g.dtype == w.dtype and torch.equal(g.view(torch.uint8), w.view(torch.uint8)) for g, w in zip(got, want)), name
