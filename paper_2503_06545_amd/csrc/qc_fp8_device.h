@@ -14,12 +14,13 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // 16 B of a row of K at any alignment, from column col on; zeros past the row's end
-template <typename XT>
+template <bool NT = false, typename XT>
 __device__ inline uint4 load_piece(const XT *xrow, int64_t col, int64_t K) {
     constexpr int E = 16 / (int)sizeof(XT);
     const int64_t past = col + E - K;   // elements of the piece past the row's end
     if (past <= 0) {
-        const u32x4_any t = *reinterpret_cast<const u32x4_any *>(xrow + col);
+        const u32x4_any *const p = reinterpret_cast<const u32x4_any *>(xrow + col);
+        const u32x4_any t = NT ? __builtin_nontemporal_load(p) : *p;
         return make_uint4(t.x, t.y, t.z, t.w);
     }
     if (past >= E) return make_uint4(0, 0, 0, 0);

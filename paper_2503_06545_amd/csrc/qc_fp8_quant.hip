@@ -16,11 +16,11 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kRowsPerWave = 8;   // eight lanes each
 
 // eight lanes' share of columns col0 .. col0 + 127 of a row of K at any alignment, zeros past its end
-template <typename XT>
+template <bool NT, typename XT>
 __device__ inline void load_block(Group<XT> &g, const XT *xrow, int64_t col0, int64_t K, int sub) {
     constexpr int E = 16 / (int)sizeof(XT), P = sizeof(g.v) / sizeof(g.v[0]);
 #pragma unroll
-    for (int j = 0; j < P; ++j) g.v[j] = load_piece(xrow, col0 + 8 * E * j + E * sub, K);
+    for (int j = 0; j < P; ++j) g.v[j] = load_piece<NT>(xrow, col0 + 8 * E * j + E * sub, K);
 }
 
 struct QuantArgs {
@@ -28,7 +28,7 @@ struct QuantArgs {
     uint8_t *qx, *qx_tiled;
     float *x_scale;
     int64_t M, K, Mp;
-    int KB, chunks;
+    int KB;
     const int32_t *offsets;   // grouped only
     Fp8Tile *map;
     int experts, tokens, map_entries, quant_blocks;
@@ -94,8 +94,10 @@ __device__ void make_map(const QuantArgs &a) {
     }
 }
 
-// A wavefront takes eight rows x GROUPS blocks of 128 columns.
-template <typename XT, int GROUPS>
+// A wavefront takes eight rows x one block of 128 columns: the shorter its chain, the shorter a small call, and the more of
+// them there are on the large ones (us at one and three blocks: 16 x 4608 2.6 3.7, 300 x 4608 binary32 4.0 6.6, 16384 x 1152 13.6
+// 16.1, 131072 x 1152 80 89, 65536 x 4608 161 169).  NT: see stream_loads().
+template <typename XT, bool NT>
 __global__ __launch_bounds__(kThreads) void fp8_quant_kernel(QuantArgs a) {
     if (a.map && (int)blockIdx.x == a.quant_blocks) {
         make_map(a);
@@ -103,47 +105,49 @@ __global__ __launch_bounds__(kThreads) void fp8_quant_kernel(QuantArgs a) {
     }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int sub = lane & 7;
-    const int64_t row_block = blockIdx.x / (uint32_t)a.chunks;
-    const int chunk = blockIdx.x % (uint32_t)a.chunks;
-    const int64_t row0 = (row_block * kWaves + wave) * kRowsPerWave, row = row0 + lane / 8;
+    const int64_t row_block = blockIdx.x / (uint32_t)a.KB;
+    const int b = blockIdx.x % (uint32_t)a.KB;
+    const int64_t row = (row_block * kWaves + wave) * kRowsPerWave + lane / 8;
     if (row >= a.M) return;
     if (a.offsets && (row < a.offsets[0] || row >= a.offsets[a.experts])) return;   // of no group
-    const XT *const xrow = reinterpret_cast<const XT *>(a.X) + row * a.K;
-    const int b0 = chunk * GROUPS;
 
-    Group<XT> g[GROUPS];
+    Group<XT> g;
+    load_block<NT>(g, reinterpret_cast<const XT *>(a.X) + row * a.K, (int64_t)b * kFp8Block, a.K, sub);
+    auto running = Group<XT>::no_max();
+    g.absmax_into(running);
+    const float s = scale_of(max_of_eight(Group<XT>::absmax_value(running)), kE4m3Most);
+    const float r = 1.0f / s;
+    uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) load_block(g[i], xrow, (int64_t)(b0 + i) * kFp8Block, a.K, sub);
-#pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-        if (b0 + i >= a.KB) break;
-        auto running = Group<XT>::no_max();
-        g[i].absmax_into(running);
-        const float s = scale_of(max_of_eight(Group<XT>::absmax_value(running)), kE4m3Most);
-        const float r = 1.0f / s;
-        uint32_t w[4];
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-            w[d] = e4m3x4(quotient(g[i].get(4 * d + 0), s, r), quotient(g[i].get(4 * d + 1), s, r),
-                          quotient(g[i].get(4 * d + 2), s, r), quotient(g[i].get(4 * d + 3), s, r));
-        const uint4 out = Group<XT>::gather_codes(w, sub);
-        const int unit = Group<XT>::unit_of(sub);
-        if (a.qx_tiled) {
-            const int64_t half = ((row / kWaveM) * a.KB + b0 + i) * 8 + (row % kWaveM) / kFragRows * 2 + unit / 4;
-            *reinterpret_cast<uint4 *>(a.qx_tiled + half * kFragBytes + (unit % 4) * 256 + (row % kFragRows) * 16) = out;
-            if (sub == 0) a.x_scale[(int64_t)(b0 + i) * a.Mp + row] = s;
+    for (int d = 0; d < 4; ++d)
+        w[d] = e4m3x4(quotient(g.get(4 * d + 0), s, r), quotient(g.get(4 * d + 1), s, r), quotient(g.get(4 * d + 2), s, r),
+                      quotient(g.get(4 * d + 3), s, r));
+    const uint4 out = Group<XT>::gather_codes(w, sub);
+    const int unit = Group<XT>::unit_of(sub);
+    if (a.qx_tiled) {
+        const int64_t half = ((row / kWaveM) * a.KB + b) * 8 + (row % kWaveM) / kFragRows * 2 + unit / 4;
+        *reinterpret_cast<uint4 *>(a.qx_tiled + half * kFragBytes + (unit % 4) * 256 + (row % kFragRows) * 16) = out;
+        if (sub == 0) a.x_scale[(int64_t)b * a.Mp + row] = s;
+    } else {
+        const int64_t col = (int64_t)b * kFp8Block + unit * kUnit;
+        uint8_t *const p = a.qx + row * a.K + col;
+        if (col + kUnit <= a.K) {
+            __builtin_memcpy(p, &out, sizeof(out));   // at any alignment
         } else {
-            const int64_t col = (int64_t)(b0 + i) * kFp8Block + unit * kUnit;
-            uint8_t *const p = a.qx + row * a.K + col;
-            if (col + kUnit <= a.K) {
-                __builtin_memcpy(p, &out, sizeof(out));   // at any alignment
-            } else {
-                const uint32_t v[4] = {out.x, out.y, out.z, out.w};
-                for (int e = 0; e < (int)(a.K - col); ++e) p[e] = (uint8_t)(v[e / 4] >> (8 * (e % 4)));
-            }
-            if (sub == 0) a.x_scale[row * a.KB + b0 + i] = s;
+            const uint32_t v[4] = {out.x, out.y, out.z, out.w};
+            for (int e = 0; e < (int)(a.K - col); ++e) p[e] = (uint8_t)(v[e / 4] >> (8 * (e % 4)));
         }
+        if (sub == 0) a.x_scale[row * a.KB + b] = s;
     }
+}
+
+// X past the caches: it is not read again, and what it would push out of the last-level cache are codes that the products are
+// about to read, from some 32 MB of it on (us, ordinary and non-temporal loads, four inputs in turn: 32 MB 13.6 12.7, binary32
+// 22.0 20.0, 604 MB 161 157; but 4 MB binary32 3.9 4.2).  Codes that stay row by row win from 200 MB of both on (131072 x 1152 82.9 78.5,
+// 65536 x 4608 170 161, 38 MB 12.3 13.6).
+bool stream_loads(int64_t x_bytes, int64_t code_bytes, bool tiled) {
+    constexpr int64_t MB = 1 << 20;
+    return tiled ? x_bytes >= 32 * MB : x_bytes + code_bytes >= 200 * MB;
 }
 
 // ---- weights ------------------------------------------------------------------------------------
@@ -207,9 +211,7 @@ hipError_t launch_fp8_quant(const void *X, qc_dtype xdt, int64_t M, int64_t K, u
     a.K = K;
     a.Mp = round_up(M, kWaveM);
     a.KB = (int)fp8_blocks(K);
-    constexpr int G = 3;
-    a.chunks = (a.KB + G - 1) / G;
-    a.quant_blocks = (int)((M + kWaves * kRowsPerWave - 1) / (kWaves * kRowsPerWave) * a.chunks);
+    a.quant_blocks = (int)((M + kWaves * kRowsPerWave - 1) / (kWaves * kRowsPerWave) * a.KB);
     a.offsets = offsets;
     a.experts = experts;
     if (map) {
@@ -218,8 +220,14 @@ hipError_t launch_fp8_quant(const void *X, qc_dtype xdt, int64_t M, int64_t K, u
         a.map_entries = (int)fp8_tiles_most(M, experts, tokens);
     }
     const dim3 grid((unsigned)(a.quant_blocks + (map ? 1 : 0))), block(kThreads);
-    if (xdt == QC_BF16) fp8_quant_kernel<uint16_t, G><<<grid, block, 0, stream>>>(a);
-    else fp8_quant_kernel<float, G><<<grid, block, 0, stream>>>(a);
+    const bool nt = stream_loads(M * K * (xdt == QC_BF16 ? 2 : 4), M * K, qx_tiled != nullptr);
+    if (xdt == QC_BF16) {
+        if (nt) fp8_quant_kernel<uint16_t, true><<<grid, block, 0, stream>>>(a);
+        else fp8_quant_kernel<uint16_t, false><<<grid, block, 0, stream>>>(a);
+    } else {
+        if (nt) fp8_quant_kernel<float, true><<<grid, block, 0, stream>>>(a);
+        else fp8_quant_kernel<float, false><<<grid, block, 0, stream>>>(a);
+    }
     return hipGetLastError();
 }
 
