@@ -51,8 +51,12 @@ __host__ inline int64_t fp8_tiles_most(int64_t M, int64_t experts, int tokens) {
     return M / tokens + (experts < M ? experts : M);
 }
 
-// workspace: [ scales: KB x Mp floats, token fastest ][ tiled codes: Mp x 128 KB ][ map of the grouped GEMM's tiles ]
-// Rows M .. Mp - 1 are neither written nor read.
+// What the GEMM copies or loads past the end of a tile's reduction, and does not use: three blocks of 128 k of the weights,
+// one of a panel of 64 tokens (and of the scales, behind which the codes lie).
+constexpr int kFp8WeightSlack = 3 * kFp8TileBytes, kFp8ActSlack = kWaveM * kFp8Block;
+
+// workspace: [ scales: KB x Mp floats, token fastest ][ tiled codes: Mp x 128 KB ][ slack ][ map of the grouped GEMM's tiles ]
+// Rows M .. Mp - 1 are not written, nor read but as part of the slack.
 struct Fp8Workspace {
     int64_t Mp, KB;
     size_t codes_offset, map_offset, total_bytes;
@@ -63,7 +67,7 @@ __host__ inline Fp8Workspace fp8_workspace(int64_t M, int64_t K) {
     w.Mp = round_up(M, kWaveM);
     w.KB = fp8_blocks(K);
     w.codes_offset = (size_t)round_up(w.Mp * w.KB * 4, 256);
-    w.map_offset = w.codes_offset + (size_t)w.Mp * (size_t)w.KB * kFp8Block;
+    w.map_offset = w.codes_offset + (size_t)w.Mp * (size_t)w.KB * kFp8Block + kFp8ActSlack;
     w.total_bytes = w.map_offset + (size_t)round_up(fp8_tiles_most(M, QC_MAX_EXPERTS, kFp8TokensLeast) * (int64_t)sizeof(Fp8Tile), 256);
     return w;
 }

@@ -94,7 +94,7 @@ qc_status linear(const void *X, qc_dtype xdt, int64_t M, int64_t K, const int32_
 extern "C" size_t qc_packed_weight_fp8_bytes(int64_t experts, int64_t N, int64_t K) {
     if (experts < 1 || N < 1 || K < 1 || experts > QC_MAX_EXPERTS || N > QC_MAX_N || K > QC_MAX_K) return 0;
     if (experts * (round_up(N, kTileN) / kTileN) * fp8_blocks(K) > kBlocksMost) return 0;
-    return (size_t)kPackedHeaderBytes + (size_t)experts * (size_t)fp8_weight_bytes(N, K);
+    return (size_t)kPackedHeaderBytes + (size_t)experts * (size_t)fp8_weight_bytes(N, K) + kFp8WeightSlack;
 }
 
 extern "C" qc_status qc_pack_weight_fp8(const float *W, int64_t experts, int64_t N, int64_t K, void *packed, float *w_scale,

@@ -63,59 +63,59 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
     const Where at = tile_of(a, v, TM);
     if (at.expert < 0) return;
     const int first = wave * (16 * MI), live = at.rows - first;   // rows of this wavefront that are stored: may be none
-    const int KB = a.KB, last = KB - 1;
+    const int KB = a.KB;
 
-    const uint8_t *const wsrc = a.w_codes + at.expert * a.w_expert_bytes + (int64_t)nt * KB * kFp8TileBytes + wave * (4 * kFragBytes);
+    // Where the next copies come from: scalar addresses that step on, and one 32-bit offset a lane, because vector registers
+    // are short and every instruction beside the products counts.  They run up to three steps past the end of the
+    // reduction, into the next tile's, or what qc_packed_weight_fp8_bytes() and fp8_workspace() add behind the last.
+    const uint8_t *wnext = a.w_codes + at.expert * a.w_expert_bytes + (int64_t)nt * KB * kFp8TileBytes + wave * (4 * kFragBytes);
+    const int64_t m0 = at.row0;
+    const uint8_t *xnext = a.x_tiled + (m0 / kWaveM) * KB * (8 * kFragBytes);
+    const float *snext = a.x_scale + m0;
     const uint32_t lane16 = lane * 16;
-    // Copies to LDS as asm, like the loads below: scalar addresses and one 32-bit offset a lane, because vector registers are
-    // short.  Lane l's piece goes to m0 + offset + its size times l; the offset counts on both sides.
-    // (s_nop: a vector instruction may have written the scalar base just before, and the compiler sees no memory instruction.)
-#define QC_COPY_16x4(at_lds, off, base)                                                                        \
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024\n\t" \
-                 "global_load_lds_dwordx4 %1, %2 offset:2048\n\tglobal_load_lds_dwordx4 %1, %2 offset:3072" ::"s"(at_lds), "v"(off), "s"(base) : "memory")
-#define QC_COPY_4(at_lds, off, base) \
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, %2" ::"s"(at_lds), "v"(off), "s"(base) : "memory")
-    const uint32_t lds_ring = (uint32_t)(uintptr_t)lds;
-    auto issue_w = [&](int step, int slot) {
-        QC_COPY_16x4(lds_ring + slot * kFp8TileBytes + wave * (4 * kFragBytes), lane16, wsrc + (int64_t)step * kFp8TileBytes);
-    };
-
-    // the channel tile's scales and biases, without a wait of their own: ahead of the first weights
-    for (int b = wave * 64; b < KB; b += kThreads)
-        QC_COPY_4((uint32_t)(uintptr_t)(lds_sw + b), 4u * min(b + lane, last), a.w_scale + ((int64_t)at.expert * a.n_tiles + nt) * KB);
-    if (wave < 2) {
-        const int n = nt * kTileN + wave * 64;
-        if (a.bias) QC_COPY_4((uint32_t)(uintptr_t)(lds_bs + wave * 64), 4u * min(lane, max((int)a.N - 1 - n, 0)), a.bias + (at.expert * a.N + min(n, (int)a.N - 1)));
-        else lds_bs[wave * 64 + lane] = 0.0f;
-    }
-
     // Rows past the last live one of the tile read that one again.  A lane's place relative to the panel of 64 tokens that
     // the tile begins in.
-    const int64_t m0 = at.row0;
-    const uint8_t *const xsrc = a.x_tiled + (m0 / kWaveM) * KB * (8 * kFragBytes);
     uint32_t xoff[MI];
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
         const int r = (int)(m0 % kWaveM) + min(first + 16 * i + c, at.rows - 1);
         xoff[i] = (uint32_t)((r / kWaveM) * KB * 8 + r % kWaveM / kFragRows * 2) * kFragBytes + h * 256 + r % kFragRows * 16;
     }
-    const float *const ssrc = a.x_scale + m0;
     const uint32_t soff = 4 * min(first + lane, at.rows - 1);
-    const uint32_t lds_sx = (uint32_t)(uintptr_t)(lds_sw + round_up(KB, kThreads)) + wave * (4 * kWaveM);   // 64 scales of this wavefront's, for two steps
+
+    // LDS: the ring, biases, the channel tile's scales, two steps of 64 token scales for each wavefront
+    const uint32_t lds_ring = (uint32_t)(uintptr_t)lds, lds_w = lds_ring + wave * (4 * kFragBytes);
+    const uint32_t lds_sx = (uint32_t)(uintptr_t)(lds_sw + round_up(KB, kThreads)) + wave * (4 * kWaveM);
+    // Copies to LDS: lane l's piece goes to m0 + offset + its size times l; the offset counts on both sides.  (s_nop: m0 has just been written.)
+#define QC_COPY_W(slot)                                                                                        \
+    do {                                                                                                       \
+        asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024\n\t" \
+                     "global_load_lds_dwordx4 %1, %2 offset:2048\n\tglobal_load_lds_dwordx4 %1, %2 offset:3072"  \
+                     ::"s"(lds_w), "v"(lane16), "s"(wnext), "n"((slot) * kFp8TileBytes) : "memory", "scc");       \
+        wnext += kFp8TileBytes;                                                                                \
+    } while (0)
+#define QC_COPY_4(at_lds, imm, off, base) \
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(at_lds), "v"(off), "s"(base), "n"(imm) : "memory", "scc")
+    // the channel tile's scales and biases, without a wait of their own: ahead of the first weights
+    for (int b = wave * 64; b < KB; b += kThreads)
+        QC_COPY_4((uint32_t)(uintptr_t)(lds_sw + b), 0, 4u * min(b + lane, KB - 1), a.w_scale + ((int64_t)at.expert * a.n_tiles + nt) * KB);
+    if (wave < 2) {
+        const int n = nt * kTileN + wave * 64;
+        if (a.bias) QC_COPY_4((uint32_t)(uintptr_t)(lds_bs + wave * 64), 0, 4u * min(lane, max((int)a.N - 1 - n, 0)), a.bias + (at.expert * a.N + min(n, (int)a.N - 1)));
+        else lds_bs[wave * 64 + lane] = 0.0f;
+    }
 
     v4i xq[2][MI][2];
-#define QC_LOAD_FIRST(dst, off, base) asm volatile("s_nop 4\n\tglobal_load_dwordx4 %0, %1, %2" : "=v"(dst) : "v"(off), "s"(base) : "memory")
 #define QC_LOAD(dst, off, base, imm) asm volatile("global_load_dwordx4 %0, %1, %2 offset:%3" : "=v"(dst) : "v"(off), "s"(base), "n"(imm) : "memory")
-#define QC_ISSUE_X(step, SLOT)                                                  \
+#define QC_ISSUE_X(SLOT)                                                        \
     do {                                                                        \
-        const uint8_t *const p_ = xsrc + (int64_t)(step) * (8 * kFragBytes);    \
-        QC_COPY_4(lds_sx + (SLOT) * (16 * kWaveM), soff, ssrc + (int64_t)(step) * a.Mp); \
-        QC_LOAD_FIRST(xq[SLOT][0][0], xoff[0], p_);                             \
-        QC_LOAD(xq[SLOT][0][1], xoff[0], p_, kFragBytes);                       \
-        _Pragma("unroll") for (int i = 1; i < MI; ++i) {                        \
-            QC_LOAD(xq[SLOT][i][0], xoff[i], p_, 0);                            \
-            QC_LOAD(xq[SLOT][i][1], xoff[i], p_, kFragBytes);                   \
+        QC_COPY_4(lds_sx, (SLOT) * (16 * kWaveM), soff, snext);                 \
+        _Pragma("unroll") for (int i = 0; i < MI; ++i) {                        \
+            QC_LOAD(xq[SLOT][i][0], xoff[i], xnext, 0);                         \
+            QC_LOAD(xq[SLOT][i][1], xoff[i], xnext, kFragBytes);                \
         }                                                                       \
+        xnext += 8 * kFragBytes;                                                \
+        snext += a.Mp;                                                          \
     } while (0)
 #define QC_WAIT_X(n, SLOT)                                                                                           \
     do {                                                                                                             \
@@ -127,15 +127,14 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
 
     // weights: wq[t % 3] the channels 8 c + t of the step; read two ahead, across the end of a step one
     v4i wq[3][2];
-    const uint32_t lds_lane = lds_ring + lane16, lds_sw_at = (uint32_t)(uintptr_t)lds_sw;
-    const uint32_t lds_sx_lane = lds_sx + h * 16;
-#define QC_READ_W(base, t)                                                                                      \
+    const uint32_t lds_lane = lds_ring + lane16, lds_sx_lane = lds_sx + h * 16;
+    uint32_t lds_sw_at = (uint32_t)(uintptr_t)lds_sw;
+#define QC_READ_W(slot, t)                                                                                      \
     do {                                                                                                        \
-        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % 3][0]) : "v"(base), "n"((t) * 2 * kFragBytes));          \
-        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % 3][1]) : "v"(base), "n"(((t) * 2 + 1) * kFragBytes));    \
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % 3][0]) : "v"(lds_lane), "n"((slot) * kFp8TileBytes + (t) * 2 * kFragBytes));          \
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % 3][1]) : "v"(lds_lane), "n"((slot) * kFp8TileBytes + ((t) * 2 + 1) * kFragBytes));    \
     } while (0)
 #define QC_WAIT_W(n, t) asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(wq[(t) % 3][0]), "+v"(wq[(t) % 3][1]) : "n"(n))
-#define QC_CLAMP(st) ((st) < last ? (st) : last)
 
     constexpr int kDeep = EXACT ? 1 : 3;
     f4 acc[MI][8];
@@ -144,17 +143,15 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
 #pragma unroll
         for (int t = 0; t < 8; ++t) acc[i][t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    int slot = 0;   // step % 3
-    auto run_step = [&](int step, auto xslot) {
-        constexpr int XS = decltype(xslot)::value;
-        const int next = slot == kSlots - 1 ? 0 : slot + 1;
-        const uint32_t here = lds_lane + slot * kFp8TileBytes, there = lds_lane + next * kFp8TileBytes;
+    // step S of six, after which ring and registers are where they were
+    auto run_step = [&](auto step_tag) {
+        constexpr int S = decltype(step_tag)::value, XS = S % 2, slot = S % kSlots, next = (S + 1) % kSlots;
         f4 sc[MI];
         float sw;
         Op x[MI];
-        QC_ISSUE_X(QC_CLAMP(step + 1), 1 - XS);
+        QC_ISSUE_X(1 - XS);
         QC_WAIT_X(4 + kXLoads, XS);
-        asm volatile("ds_read_b32 %0, %1" : "=v"(sw) : "v"(lds_sw_at + 4 * step));
+        asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(sw) : "v"(lds_sw_at), "n"(4 * S));
 #pragma unroll
         for (int i = 0; i < MI; ++i)
             asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(sc[i]) : "v"(lds_sx_lane), "n"(XS * 16 * kWaveM + 64 * i));
@@ -166,15 +163,15 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
         for (int n = 0; n < 8 * MI + kDeep; ++n) {
             const int t = n / MI, i = n % MI;
             if (i == 0 && t < 8) {
-                if (t < 6) QC_READ_W(here, t + 2);
+                if (t < 6) QC_READ_W(slot, t + 2);
                 if (t == 0) QC_WAIT_W(2 + MI + 1 + 2, 0);
                 else if (t == 6) {   // tiles 6 and 7 are in registers: this wavefront is done with the slot
                     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(wq[0][0]), "+v"(wq[0][1]), "+v"(wq[1][0]), "+v"(wq[1][1]));
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
-                    issue_w(QC_CLAMP(step + 3), slot);
+                    QC_COPY_W(slot);
                 } else if (t == 7) {
-                    QC_READ_W(there, 0);
+                    QC_READ_W(next, 0);
                 } else {
                     QC_WAIT_W(4, t);
                 }
@@ -196,37 +193,47 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        QC_READ_W(there, 1);
-        slot = next;
+        QC_READ_W(next, 1);
     };
 
-    issue_w(0, 0);
-    QC_ISSUE_X(0, 0);
-    issue_w(QC_CLAMP(1), 1);
-    issue_w(QC_CLAMP(2), 2);
+    // (a vector instruction may have written a scalar address just before, and the compiler sees no memory instruction)
+    asm volatile("s_nop 4" ::"s"(wnext), "s"(xnext), "s"(snext));
+    QC_COPY_W(0);
+    QC_ISSUE_X(0);
+    QC_COPY_W(1);
+    QC_COPY_W(2);
     QC_WAIT_VMCNT(kXLoads + 8);   // W(0) has landed
-    __syncthreads();             // and everybody else's, with the scales
-    QC_READ_W(lds_lane, 0);
-    QC_READ_W(lds_lane, 1);
-    int step = 0;
-    for (; step + 2 <= KB; step += 2) {
-        run_step(step, std::integral_constant<int, 0>{});
-        run_step(step + 1, std::integral_constant<int, 1>{});
+    __syncthreads();              // and everybody else's, with the scales
+    QC_READ_W(0, 0);
+    QC_READ_W(0, 1);
+#define QC_STEP(S) run_step(std::integral_constant<int, S>{})
+    int left = KB;
+    for (; left >= 6; left -= 6) {
+        QC_STEP(0);
+        QC_STEP(1);
+        QC_STEP(2);
+        QC_STEP(3);
+        QC_STEP(4);
+        QC_STEP(5);
+        lds_sw_at += 24;
     }
-    if (step < KB) run_step(step, std::integral_constant<int, 0>{});
+    if (left > 0) QC_STEP(0);
+    if (left > 1) QC_STEP(1);
+    if (left > 2) QC_STEP(2);
+    if (left > 3) QC_STEP(3);
+    if (left > 4) QC_STEP(4);
+#undef QC_STEP
     // drain what is in flight before its registers are used for anything else
     QC_WAIT_X(0, 0);
     QC_WAIT_X(0, 1);
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(wq[0][0]), "+v"(wq[0][1]), "+v"(wq[1][0]), "+v"(wq[1][1]));
-#undef QC_CLAMP
 #undef QC_WAIT_W
 #undef QC_READ_W
 #undef QC_WAIT_X
 #undef QC_ISSUE_X
 #undef QC_LOAD
-#undef QC_LOAD_FIRST
 #undef QC_COPY_4
-#undef QC_COPY_16x4
+#undef QC_COPY_W
 
     // ---- epilogue: lane (c, h) holds channels 8 c .. + 7 of tokens 16 i + 4 h + q
     const int64_t n0 = (int64_t)nt * kTileN + 8 * c;

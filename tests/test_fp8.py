@@ -65,8 +65,9 @@ def test_oracle_linear_is_the_dequantized_product():
 # ---- sizes and refusals --------------------------------------------------------------------------
 
 def test_size_queries():
-    assert qc.qc_packed_weight_fp8_bytes(1, 3456, 1152) == 256 + 3456 * 1152
-    assert qc.qc_packed_weight_fp8_bytes(5, 200, 100) == 256 + 5 * 256 * 128
+    # a header, whole blocks of 128 x 128, and three more of them that the GEMM runs past the last one
+    assert qc.qc_packed_weight_fp8_bytes(1, 3456, 1152) == 256 + 3456 * 1152 + 3 * 16384
+    assert qc.qc_packed_weight_fp8_bytes(5, 200, 100) == 256 + 5 * 256 * 128 + 3 * 16384
     for bad in ((0, 8, 8), (1, 0, 8), (1, 8, 0), (qc.QC_MAX_EXPERTS + 1, 8, 8), (1, qc.QC_MAX_N + 1, 8), (1, 8, qc.QC_MAX_K + 1),
                 (1024, 1 << 24, 1 << 16)):
         assert qc.qc_packed_weight_fp8_bytes(*bad) == 0
