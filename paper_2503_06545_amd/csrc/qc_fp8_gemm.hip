@@ -39,8 +39,8 @@ constexpr int kRingBytes = kSlots * kFp8TileBytes;
 // makes valid.  Vector memory operations complete in order, which is the scales and biases, W(0) X(0) W(1) W(2), then X(s + 1)
 // at the start and W(s + 3) towards the end of step s, where X are the activations with their scales.  The wait for X(s), after X(s + 1)
 // has been requested, leaves that and W(s + 2) in flight, so W(s + 1) has landed with it; the barrier before channel
-// block 6 then makes the next step's weights readable and the slot of this one's free, whose last reads are in registers by then.
-// Past the last step the index is clamped: those copies repeat data that is not used again.
+// block 6 or 7 then makes the next step's weights readable and the slot of this one's free, whose last reads are in registers by then.
+// The copies of the last steps run past the reduction and are not used.
 //
 // What bounds it on large problems is power: 8192 x 8192 x 8192 runs at 1.7 of 2.4 GHz with the matrix units 60 % busy, where a
 // loop on registers alone, each product scaled and added, holds 1.9 GHz, 94 % and 3760 TFLOP/s.  us for 131072 x 1152 x 4608,
@@ -89,9 +89,10 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
     // Copies to LDS: lane l's piece goes to m0 + offset + its size times l; the offset counts on both sides.  (s_nop: m0 has just been written.)
 #define QC_COPY_W(slot)                                                                                        \
     do {                                                                                                       \
-        asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024\n\t" \
-                     "global_load_lds_dwordx4 %1, %2 offset:2048\n\tglobal_load_lds_dwordx4 %1, %2 offset:3072"  \
-                     ::"s"(lds_w), "v"(lane16), "s"(wnext), "n"((slot) * kFp8TileBytes) : "memory", "scc");       \
+        asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:%4\n\t" \
+                     "global_load_lds_dwordx4 %1, %2 offset:%5\n\tglobal_load_lds_dwordx4 %1, %2 offset:%6"    \
+                     ::"s"(lds_w), "v"(lane16), "s"(wnext), "n"((slot) * kFp8TileBytes), "n"(kFragBytes), "n"(2 * kFragBytes), \
+                     "n"(3 * kFragBytes) : "memory", "scc");                                                   \
         wnext += kFp8TileBytes;                                                                                \
     } while (0)
 #define QC_COPY_4(at_lds, imm, off, base) \
@@ -125,18 +126,19 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
     } while (0)
     constexpr int kXLoads = 2 * MI + 1;
 
-    // weights: wq[t % 3] the channels 8 c + t of the step; read two ahead, across the end of a step one
-    v4i wq[3][2];
+    // weights: wq[t % TB] the channels 8 c + t of the step; read two ahead, across the end of a step one, or, for want of registers, one
+    constexpr int TB = MI == 4 ? 2 : 3;
+    v4i wq[TB][2];
     const uint32_t lds_lane = lds_ring + lane16, lds_sx_lane = lds_sx + h * 16;
     uint32_t lds_sw_at = (uint32_t)(uintptr_t)lds_sw;
 #define QC_READ_W(slot, t)                                                                                      \
     do {                                                                                                        \
-        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % 3][0]) : "v"(lds_lane), "n"((slot) * kFp8TileBytes + (t) * 2 * kFragBytes));          \
-        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % 3][1]) : "v"(lds_lane), "n"((slot) * kFp8TileBytes + ((t) * 2 + 1) * kFragBytes));    \
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % TB][0]) : "v"(lds_lane), "n"((slot) * kFp8TileBytes + (t) * 2 * kFragBytes));          \
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(wq[(t) % TB][1]) : "v"(lds_lane), "n"((slot) * kFp8TileBytes + ((t) * 2 + 1) * kFragBytes));    \
     } while (0)
-#define QC_WAIT_W(n, t) asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(wq[(t) % 3][0]), "+v"(wq[(t) % 3][1]) : "n"(n))
+#define QC_WAIT_W(n, t) asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(wq[(t) % TB][0]), "+v"(wq[(t) % TB][1]) : "n"(n))
 
-    constexpr int kDeep = EXACT ? 1 : 3;
+    constexpr int kDeep = EXACT ? 1 : MI == 4 ? 1 : 3;
     f4 acc[MI][8];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
@@ -163,20 +165,34 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
         for (int n = 0; n < 8 * MI + kDeep; ++n) {
             const int t = n / MI, i = n % MI;
             if (i == 0 && t < 8) {
-                if (t < 6) QC_READ_W(slot, t + 2);
-                if (t == 0) QC_WAIT_W(2 + MI + 1 + 2, 0);
-                else if (t == 6) {   // tiles 6 and 7 are in registers: this wavefront is done with the slot
-                    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(wq[0][0]), "+v"(wq[0][1]), "+v"(wq[1][0]), "+v"(wq[1][1]));
-                    __builtin_amdgcn_s_barrier();
-                    asm volatile("" ::: "memory");
-                    QC_COPY_W(slot);
-                } else if (t == 7) {
-                    QC_READ_W(next, 0);
+                if constexpr (TB == 3) {
+                    if (t < 6) QC_READ_W(slot, t + 2);
+                    if (t == 0) QC_WAIT_W(2 + MI + 1 + 2, 0);
+                    else if (t == 6) {   // blocks 6 and 7 are in registers: this wavefront is done with the slot
+                        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(wq[0][0]), "+v"(wq[0][1]), "+v"(wq[1][0]), "+v"(wq[1][1]));
+                        __builtin_amdgcn_s_barrier();
+                        asm volatile("" ::: "memory");
+                        QC_COPY_W(slot);
+                    } else if (t == 7) {
+                        QC_READ_W(next, 0);
+                    } else {
+                        QC_WAIT_W(4, t);
+                    }
                 } else {
-                    QC_WAIT_W(4, t);
+                    if (t < 7) QC_READ_W(slot, t + 1);
+                    if (t == 0) QC_WAIT_W(MI + 3, 0);
+                    else if (t == 7) {
+                        QC_WAIT_W(0, 7);
+                        __builtin_amdgcn_s_barrier();
+                        asm volatile("" ::: "memory");
+                        QC_COPY_W(slot);
+                        QC_READ_W(next, 0);
+                    } else {
+                        QC_WAIT_W(2, t);
+                    }
                 }
             }
-            if (t < 8) p[n % (kDeep + 1)] = product(x[i], Op(wq[t % 3][0], wq[t % 3][1]));
+            if (t < 8) p[n % (kDeep + 1)] = product(x[i], Op(wq[t % TB][0], wq[t % TB][1]));
             __builtin_amdgcn_sched_barrier(0);
             if (n == kDeep) {
                 asm volatile("s_waitcnt lgkmcnt(2)" : "+v"(sw));
@@ -193,7 +209,7 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        QC_READ_W(next, 1);
+        if constexpr (TB == 3) QC_READ_W(next, 1);
     };
 
     // (a vector instruction may have written a scalar address just before, and the compiler sees no memory instruction)
@@ -205,7 +221,7 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
     QC_WAIT_VMCNT(kXLoads + 8);   // W(0) has landed
     __syncthreads();              // and everybody else's, with the scales
     QC_READ_W(0, 0);
-    QC_READ_W(0, 1);
+    if constexpr (TB == 3) QC_READ_W(0, 1);
 #define QC_STEP(S) run_step(std::integral_constant<int, S>{})
     int left = KB;
     for (; left >= 6; left -= 6) {
@@ -296,23 +312,25 @@ hipError_t launch_tiles(const Fp8GemmArgs &a, qc_epilogue epi, hipStream_t strea
 constexpr int kCus = 256;
 
 // What a CU takes for a step of `per_cu` of the ring kernel's tiles of 64 h tokens, in hundredths of a microsecond, read off
-// linears of 300 to 20000 tokens at every height.  A tile that a CU has to itself waits out its own loads, which a lower one has
-// fewer of; from two or three on the products count, and for binary32 outputs their widening.  (us at 192 / 128 / 64 tokens:
-// 300 x 4608 x 1152 31.3 25.2 20.2, 2400 x 4608 x 1152 37.7 31.6 32.3, 5000 x 4608 x 1152 46.0 49.2 51.3, 5000 x 1152 x 4608 41.5 39.8
-// 47.0, 20000 x 1152 x 4608 126 130 162; binary32, 128 / 64: 300 x 4608 x 1152 46.0 34.7, 4099 x 1000 x 1301 31.3 28.8, 10000 x
-// 1152 x 4608 132 144.)
-static double step_cost(int h, double per_cu, bool exact, bool lengthy) {
+// linears of 300 to 60000 tokens at every height; by it a call takes 1.8 % longer than at its best one, at 128 tokens always 3.5 %, at
+// 192 6.6 %.  A tile that a CU has to itself waits out its own loads, which a lower one has fewer of; from two or three on the
+// products count, and for binary32 outputs their widening; and on calls that go on for long, where power does, what a
+// higher tile moves less for each product.  (us at 256 / 192 / 128 / 64 tokens: 300 x 4608 x 1152 - 31.3 25.2 20.2, 5000 x 1152 x 4608 -
+// 41.5 39.8 47.0, 33199 x 1152 x 4608 203 199 203 264, 65536 x 4608 x 1152 450 462 481; binary32, 128 / 64: 300 x 4608 x 1152
+// 46.0 34.7, 4099 x 1000 x 1301 31.3 28.8, 10000 x 1152 x 4608 132 144.)
+static double step_cost(int h, double per_cu, bool exact) {
     if (exact) return h == 1 ? (per_cu <= 1 ? 85 : per_cu <= 2 ? 140 : 68 * per_cu) : per_cu <= 1 ? 115 : per_cu <= 2 ? 210 : 120 * per_cu;
-    if (h == 1) return per_cu <= 1 ? 45 : per_cu <= 2 ? 69 : (lengthy ? 44 : 37) * per_cu;
-    if (h == 2) return per_cu <= 1 ? 60 : per_cu <= 2 ? 110 : 60 * per_cu;
-    return per_cu <= 1 ? 85 : 88 * per_cu;
+    if (h == 1) return per_cu <= 1 ? 45 : per_cu <= 2 ? 69 : 42 * per_cu;
+    if (h == 2) return per_cu <= 1 ? 60 : per_cu <= 2 ? 95 : 60 * per_cu;
+    if (h == 3) return per_cu <= 1 ? 85 : 84 * per_cu;
+    return per_cu <= 1 ? 108 : (per_cu < 12 ? 122 : 110) * per_cu;
 }
 
-static int ring_tokens(int64_t M, int64_t N, int experts, bool grouped, bool exact, bool lengthy) {
+static int ring_tokens(int64_t M, int64_t N, int experts, bool grouped, bool exact) {
     const int64_t n_tiles = round_up(N, kTileN) / kTileN;
     int best = 0;
     double least = 0;
-    for (int h = exact ? 2 : 3; h >= 1; --h) {
+    for (int h = exact ? 2 : 4; h >= 1; --h) {
         double per_cu;
         if (grouped) {   // half a tile more than its rows fill for each expert that has any
             const double live = (double)(experts < M ? experts : M), each = (double)M / live / (64 * h) + 0.5;
@@ -321,7 +339,7 @@ static int ring_tokens(int64_t M, int64_t N, int experts, bool grouped, bool exa
             const int64_t tiles = (M + 64 * h - 1) / (64 * h) * n_tiles;
             per_cu = tiles <= 4 * kCus ? (double)((tiles + kCus - 1) / kCus) : (double)tiles / kCus;
         }
-        const double cost = step_cost(h, per_cu, exact, lengthy);
+        const double cost = step_cost(h, per_cu, exact);
         if (best == 0 || cost < least) { best = h; least = cost; }
     }
     return 64 * best;
@@ -349,7 +367,7 @@ Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, int experts, bool grouped, qc_
             p.few = {32, 4};
         }
     }
-    p.tokens = p.few.tokens ? p.few.tokens : ring_tokens(M, N, experts, grouped, exact, lengthy);
+    p.tokens = p.few.tokens ? p.few.tokens : ring_tokens(M, N, experts, grouped, exact);
     return p;
 }
 
@@ -357,6 +375,7 @@ hipError_t launch_fp8_gemm(const Fp8GemmArgs &args, int tokens, qc_epilogue epi,
     if (ydt == QC_OUT_F32) return tokens == 64 ? launch_tiles<1, QC_OUT_F32>(args, epi, stream) : launch_tiles<2, QC_OUT_F32>(args, epi, stream);
     if (tokens == 64) return launch_tiles<1, QC_OUT_BF16>(args, epi, stream);
     if (tokens == 128) return launch_tiles<2, QC_OUT_BF16>(args, epi, stream);
+    if (tokens == 256) return launch_tiles<4, QC_OUT_BF16>(args, epi, stream);
     return launch_tiles<3, QC_OUT_BF16>(args, epi, stream);
 }
 

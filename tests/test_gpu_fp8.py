@@ -178,37 +178,62 @@ def which(M, K, N, out, experts=0):
     return p["kernel"], p["tokens"], p["channels"], p["fused"]
 
 
-KERNELS = [("few", 16, 16, True), ("few", 16, 32, True), ("few", 16, 64, True), ("few", 32, 64, False), ("ring", 64, 128, False),
-           ("ring", 128, 128, False)]
+# (kernel, tokens, channels, fused), a ragged reduction and channels, and whether the output may be binary32
+KERNELS = [(("few", 16, 16, True), 700, 700, 2), (("few", 16, 32, True), 1153, 2311, 2), (("few", 16, 64, True), 513, 4609, 2),
+           (("few", 32, 64, False), 5001, 700, 2), (("ring", 64, 128, False), 260, 1300, 2), (("ring", 128, 128, False), 130, 1301, 2),
+           (("ring", 192, 128, False), 257, 701, 1), (("ring", 256, 128, False), 385, 6901, 1)]
 
 
-@pytest.mark.parametrize("x", ["bf16", "f32"])
-@pytest.mark.parametrize("M,K,N,out,kernel", [
-    (5, 700, 700, "f32", 0), (5, 700, 700, "bf16", 0), (20, 1153, 2311, "f32", 1), (20, 1153, 2311, "bf16", 1), (70, 513, 4609, "f32", 2), (70, 513, 4609, "bf16", 2),
-    (150, 5001, 700, "f32", 3), (150, 5001, 700, "bf16", 3), (550, 260, 2200, "f32", 4), (550, 260, 2200, "bf16", 4),
-    (16500, 130, 1301, "f32", 5), (1500, 384, 5100, "bf16", 5), (20500, 257, 1301, "bf16", 6)])
-def test_every_kernel_at_ragged_sizes(M, K, N, out, kernel, x):
-    assert which(M, K, N, out) == (KERNELS + [("ring", 192, 128, False)])[kernel]
-    run_linear(np.random.default_rng(kernel), M, K, N, x, out, bias=kernel % 2 == 0)
+def tokens_for(kernel, K, N, out, experts=0):
+    """The fewest tokens of a list, odd ones, for which a linear of these sizes takes this kernel."""
+    sizes = sorted({int(1.19 ** i) | 1 for i in range(63)})
+    found = [M for M in sizes if which(M, K, N, out, experts) == kernel]
+    assert found, (kernel, K, N, out, experts)
+    return found[0]
 
 
-@pytest.mark.parametrize("M,K,N,E,out,kernel", [(9, 200, 1000, 4, "f32", 1), (40, 300, 2000, 5, "bf16", 2), (100, 5001, 130, 3, "bf16", 3), (100, 5001, 130, 3, "f32", 3),
-                                                (600, 300, 1300, 6, "bf16", 4), (600, 300, 1300, 6, "f32", 4), (16000, 130, 1000, 64, "bf16", 5),
-                                                (20000, 130, 701, 2, "f32", 5), (3300, 257, 3301, 2, "bf16", 6)])
-def test_every_kernel_grouped(M, K, N, E, out, kernel):
-    assert which(M, K, N, out, E) == (KERNELS + [("ring", 192, 128, False)])[kernel]
-    rng = np.random.default_rng(kernel + M)
-    cut = sorted(int(v) for v in rng.integers(0, M, size=E))
-    run_grouped(rng, M, K, N, [0, *cut], "bf16", out)
+@pytest.mark.parametrize("x,out", [("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("kernel", range(len(KERNELS)))
+def test_every_kernel_at_ragged_sizes(kernel, x, out):
+    what, K, N, outs = KERNELS[kernel]
+    if outs == 1 and out == "f32":
+        pytest.skip("binary32 outputs have no tiles of this height")
+    M = tokens_for(what, K, N, out)
+    if M < 10000:
+        run_linear(np.random.default_rng(kernel), M, K, N, x, out, bias=kernel % 2 == 0)
+    else:
+        run_repeated(np.random.default_rng(kernel), M, K, N, x, out)
 
 
-# the sizes of real layers, sampled: the rows of a small block repeated, every row against the block's
-@pytest.mark.parametrize("M,K,N,out,epi", [(16384, 1152, 3456, "bf16", "none"), (20000, 4608, 1152, "f32", "none"), (9000, 1152, 4608, "bf16", "gelu_tanh"),
-                                           (4099, 1000, 1301, "f32", "gelu_erf"), (2500, 9216, 640, "bf16", "none"), (700000, 128, 3200, "bf16", "none")])
-def test_large_linears(M, K, N, out, epi):
-    rng = np.random.default_rng(M + N)
-    period = 48
-    W, X = weights(rng, N, K), random_x(rng, period, K, "bf16")
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("kernel", range(len(KERNELS)))
+def test_every_kernel_grouped(kernel, out):
+    what, K, N, outs = KERNELS[kernel]
+    if outs == 1 and out == "f32":
+        pytest.skip("binary32 outputs have no tiles of this height")
+    E = 3
+    M = tokens_for(what, K, N, out, E)
+    rng = np.random.default_rng(kernel)
+    if M < 10000:
+        cut = sorted(int(v) for v in rng.integers(0, M + 1, size=E))
+        run_grouped(rng, M, K, N, [0, *cut], "bf16", out)
+    else:
+        run_repeated_groups(rng, [M // 3 + 1, 0, M - 2 * (M // 3)], K, N, out)
+
+
+@pytest.mark.parametrize("blocks", range(1, 14))
+def test_every_length_of_the_rings_last_steps(blocks):
+    """Six steps to a turn of the ring, and what is left of one."""
+    K = 128 * blocks - blocks % 3
+    for what, out in ((("ring", 64, 128, False), "f32"), (("ring", 128, 128, False), "bf16"), (("ring", 192, 128, False), "bf16"), (("ring", 256, 128, False), "bf16")):
+        N = 6901 if what[1] == 256 else 301
+        run_repeated(np.random.default_rng(blocks), tokens_for(what, K, N, out), K, N, "bf16", out)
+
+
+def run_repeated(rng, M, K, N, x="bf16", out="bf16", epi="none"):
+    """Many tokens: the rows of a small block repeated, the block against the oracle and every row against the block's."""
+    period = min(M, 47)
+    W, X = weights(rng, N, K), random_x(rng, period, K, x)
     ref = oracle.qlinear_fp8(X, *oracle.quant_weight_fp8(W), None, EPIS[epi])
     Xd = dev(X).repeat(-(-M // period), 1)[:M].contiguous()
     Y = qc.qlinear_fp8_t(Xd, qc.pack_weight_fp8_t(dev(W)), None, epi, out)
@@ -217,6 +242,30 @@ def test_large_linears(M, K, N, out, epi):
     assert bool((Y[:whole].view(-1, period, N) == Y[:period]).all())
     if M > whole:
         assert torch.equal(Y[whole:], Y[:M - whole])
+
+
+def run_repeated_groups(rng, sizes, K, N, out="bf16"):
+    period = 50
+    offsets = np.concatenate([[0], np.cumsum(sizes)]).tolist()
+    W = np.stack([weights(rng, N, K) for _ in sizes])
+    X = random_x(rng, period, K, "bf16")
+    Xd = torch.cat([dev(X).repeat(-(-n // period), 1)[:n] for n in sizes])
+    off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    Y = qc.qlinear_fp8_grouped_t(Xd, qc.pack_weight_fp8_t(dev(W)), off, out=out)
+    for e, n in enumerate(sizes):
+        if n:
+            ref = oracle.qlinear_fp8(X, *oracle.quant_weight_fp8(W[e]))
+            y = Y[offsets[e]:offsets[e + 1]]
+            assert_within(host_f64(y[:period]), ref, K, out, "none")
+            assert torch.equal(y, y[:period].repeat(-(-n // period), 1)[:n])
+
+
+# the sizes of real layers, sampled
+@pytest.mark.parametrize("M,K,N,out,epi", [(16384, 1152, 3456, "bf16", "none"), (20000, 4608, 1152, "f32", "none"), (9000, 1152, 4608, "bf16", "gelu_tanh"),
+                                           (40000, 1152, 4608, "bf16", "gelu_tanh"), (4099, 1000, 1301, "f32", "gelu_erf"),
+                                           (2500, 9216, 640, "bf16", "none"), (700000, 128, 3200, "bf16", "none")])
+def test_large_linears(M, K, N, out, epi):
+    run_repeated(np.random.default_rng(M + N), M, K, N, "bf16", out, epi)
 
 
 def test_special_values_stay_in_their_token():
@@ -303,21 +352,8 @@ def test_as_many_experts_as_there_may_be(rows_each):
 
 
 def test_large_groups():
-    """Groups of many tiles: the rows of a small block repeated within each group."""
-    rng = np.random.default_rng(2)
-    K, N, sizes, period = 1152, 640, [5000, 0, 9001, 130, 2700], 50
-    offsets = np.concatenate([[0], np.cumsum(sizes)]).tolist()
-    W = np.stack([weights(rng, N, K) for _ in sizes])
-    X = random_x(rng, period, K, "bf16")
-    Xd = torch.cat([dev(X).repeat(-(-n // period), 1)[:n] for n in sizes])
-    off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
-    Y = qc.qlinear_fp8_grouped_t(Xd, qc.pack_weight_fp8_t(dev(W)), off)
-    for e, n in enumerate(sizes):
-        if n:
-            ref = oracle.qlinear_fp8(X, *oracle.quant_weight_fp8(W[e]))
-            y = Y[offsets[e]:offsets[e + 1]]
-            assert_within(host_f64(y[:period]), ref, K, "bf16", "none")
-            assert torch.equal(y, y[:period].repeat(-(-n // period), 1)[:n])
+    """Groups of many tiles."""
+    run_repeated_groups(np.random.default_rng(2), [5000, 0, 9001, 130, 2700], 1152, 640)
 
 
 def test_one_group_is_the_linear():
