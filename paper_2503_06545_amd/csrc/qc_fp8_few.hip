@@ -283,14 +283,17 @@ hipError_t launch_few_tile(const FewArgs &a, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// the tiles that fp8_plan() makes: 32 x 64 from codes, 16 x 16, 32 or 64 from X
 template <int SRC, int OUT>
 hipError_t launch_few_shape(const FewArgs &a, Fp8FewTile tile, hipStream_t stream) {
     if constexpr (SRC == kFromCodes) {
-        if (tile.tokens == 32) return tile.frags == 4 ? launch_few_tile<SRC, OUT, 2, 4>(a, stream) : launch_few_tile<SRC, OUT, 2, 2>(a, stream);
+        return tile.tokens == 32 && tile.frags == 4 ? launch_few_tile<SRC, OUT, 2, 4>(a, stream) : hipErrorInvalidValue;
+    } else {
+        if (tile.tokens != 16) return hipErrorInvalidValue;
+        if (tile.frags == 1) return launch_few_tile<SRC, OUT, 1, 1>(a, stream);
+        if (tile.frags == 2) return launch_few_tile<SRC, OUT, 1, 2>(a, stream);
+        return launch_few_tile<SRC, OUT, 1, 4>(a, stream);
     }
-    if (tile.frags == 1) return launch_few_tile<SRC, OUT, 1, 1>(a, stream);
-    if (tile.frags == 2) return launch_few_tile<SRC, OUT, 1, 2>(a, stream);
-    return launch_few_tile<SRC, OUT, 1, 4>(a, stream);
 }
 
 }  // namespace

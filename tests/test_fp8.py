@@ -152,7 +152,7 @@ def test_plans():
     assert plan(1, 4608, 1152)["channels"] == 16 and plan(130, 1152, 1152)["channels"] == 64
     assert plan(300, 4608, 1152) == {"kernel": "few", "tokens": 32, "channels": 64, "fused": False}
     assert plan(600, 4608, 1152, "f32")["kernel"] == "few" and plan(600, 4608, 1152)["kernel"] == "ring"
-    assert plan(131072, 1152, 4608) == {"kernel": "ring", "tokens": 192, "channels": 128, "fused": False}
+    assert plan(131072, 1152, 4608) == {"kernel": "ring", "tokens": 256, "channels": 128, "fused": False}
     assert plan(131072, 1152, 4608, "f32")["tokens"] == 128 and plan(1200, 1152, 1152)["tokens"] == 64
     assert plan(8, 4608, 1152, experts=32)["fused"] and plan(200, 1152, 4608, experts=32)["tokens"] == 64
     assert plan(16000, 1152, 4608, experts=64)["tokens"] == 128
