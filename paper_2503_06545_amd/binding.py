@@ -793,6 +793,14 @@ def _fp8_operand(t, name, dtypes, shape, device=None) -> None:
         raise ValueError(f"{name} must be on the current GPU, got {t.device}")
 
 
+def _fp8_weight(pw) -> None:
+    torch = _torch()
+    _fp8_operand(pw.blob, "pw.blob", (torch.uint8,), (None,))
+    if pw.blob.numel() < qc_packed_weight_fp8_bytes(pw.experts, pw.N, pw.K):
+        raise ValueError(f"pw.blob holds {pw.blob.numel()} bytes, too few for {pw.experts} x {pw.N} x {pw.K}")
+    _fp8_operand(pw.scale, "pw.scale", (torch.float32,), (pw.experts, -(-pw.N // QC_FP8_BLOCK), -(-pw.K // QC_FP8_BLOCK)))
+
+
 def _fp8_activation(X, K=None) -> None:
     torch = _torch()
     _fp8_operand(X, "X", (torch.float32, torch.bfloat16), (None, K))
@@ -815,6 +823,7 @@ def pack_weight_fp8_t(W) -> PackedWeightFp8:
 def unpack_weight_codes_fp8_t(pw: PackedWeightFp8):
     """The codes, float8_e4m3fn [experts, N, K]."""
     torch = _torch()
+    _fp8_weight(pw)
     codes = torch.empty((pw.experts, pw.N, pw.K), dtype=torch.uint8, device=pw.blob.device)
     _check(qc_unpack_weight_codes_fp8(pw.blob.data_ptr(), pw.experts, pw.N, pw.K, codes.data_ptr(), _stream()),
            "qc_unpack_weight_codes_fp8")
@@ -851,8 +860,7 @@ def qlinear_fp8_workspace_t(M: int, K: int, N: int, device="cuda"):
 def _fp8_linear_operands(X, pw, bias, out, workspace, Y, bias_shape):
     torch = _torch()
     _fp8_activation(X, pw.K)
-    _fp8_operand(pw.blob, "pw.blob", (torch.uint8,), (None,))
-    _fp8_operand(pw.scale, "pw.scale", (torch.float32,), (pw.experts, -(-pw.N // QC_FP8_BLOCK), -(-pw.K // QC_FP8_BLOCK)))
+    _fp8_weight(pw)
     ydtype = {"f32": torch.float32, "bf16": torch.bfloat16}[out]
     if bias is not None:
         _fp8_operand(bias, "bias", (torch.float32,), bias_shape)
@@ -898,10 +906,10 @@ _PER_STEP = ("qlinear_t", "qlinear_asym_t", "qlinear_tensor_t", "latent_delta_t"
 
 
 def _entries():
-    """The addresses of the C entries behind _PER_STEP, in that order, and of the rotated linear."""
+    """The addresses of the C entries behind _PER_STEP, in that order, and of the rotated linear and a blob's size."""
     names = ("qc_qlinear_act_bits", "qc_qlinear_asym", "qc_qlinear_tensor", "qc_latent_delta", "qc_layer_similarity",
              "qc_frame_gradient_norm", "qc_cumulative_variation", "qc_quant_act_fp8", "qc_qlinear_fp8", "qc_qlinear_fp8_grouped",
-             "qc_qlinear_rot")
+             "qc_qlinear_rot", "qc_packed_weight_fp8_bytes")
     return tuple(ctypes.cast(getattr(lib(), n), ctypes.c_void_p).value for n in names)
 
 

@@ -40,7 +40,7 @@ PyObject *attr_blob, *attr_scale, *attr_N, *attr_K, *attr_bits, *attr_experts;
 // what one import of the module holds; the C entries are asked for on the first call
 struct State {
     PyObject *resolve, *check, *fallback[kHelpers];
-    void *entry[kHelpers + 1];   // the last one: qc_qlinear_rot
+    void *entry[kHelpers + 2];   // the last two: qc_qlinear_rot, qc_packed_weight_fp8_bytes
     bool resolved;
 };
 State *state_of(PyObject *module) { return static_cast<State *>(PyModule_GetState(module)); }
@@ -49,8 +49,8 @@ bool resolve_entries(State *s) {
     if (s->resolved) return true;
     PyObject *addresses = s->resolve ? PyObject_CallNoArgs(s->resolve) : nullptr;
     if (!addresses) return false;
-    bool ok = PyTuple_Check(addresses) && PyTuple_GET_SIZE(addresses) == kHelpers + 1;
-    for (int i = 0; ok && i <= kHelpers; ++i) {
+    bool ok = PyTuple_Check(addresses) && PyTuple_GET_SIZE(addresses) == kHelpers + 2;
+    for (int i = 0; ok && i < kHelpers + 2; ++i) {
         s->entry[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(addresses, i));
         ok = s->entry[i] != nullptr;
     }
@@ -399,7 +399,8 @@ bool linear_fp8(const Call &c, int at, PyObject *offsets_object, PyObject *&resu
     {
         PyObject *const b = PyObject_GetAttr(pw, attr_blob), *const s = b ? PyObject_GetAttr(pw, attr_scale) : nullptr;
         const at::Tensor *const tb = tensor(b), *const ts = tensor(s);
-        const bool ok = tb && ts && operand(*tb, at::kByte, {tb->numel()}, device) &&
+        const auto bytes_of = reinterpret_cast<decltype(&qc_packed_weight_fp8_bytes)>(c.s->entry[kHelpers + 1]);
+        const bool ok = tb && ts && operand(*tb, at::kByte, {tb->numel()}, device) && (size_t)tb->numel() >= bytes_of(experts, N, K) &&
                         operand(*ts, at::kFloat, {experts, blocks_of(N), blocks_of(K)}, device);
         blob = ok ? tb->data_ptr() : nullptr;
         scale = ok ? static_cast<const float *>(ts->data_ptr()) : nullptr;
@@ -440,7 +441,7 @@ PyObject *qlinear_fp8_grouped_t(PyObject *m, PyObject *const *args, Py_ssize_t n
 }
 
 // setup(resolve, check, (the Python helpers, in the order of Helper)).  resolve() -> the addresses of the C entries, in
-// that order and qc_qlinear_rot last; check(status, where) raises.
+// that order, then qc_qlinear_rot's and qc_packed_weight_fp8_bytes'; check(status, where) raises.
 PyObject *setup(PyObject *module, PyObject *args) {
     PyObject *resolve, *check, *helpers;
     if (!PyArg_ParseTuple(args, "OOO!", &resolve, &check, &PyTuple_Type, &helpers)) return nullptr;

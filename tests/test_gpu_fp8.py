@@ -268,6 +268,11 @@ def test_large_linears(M, K, N, out, epi):
     run_repeated(np.random.default_rng(M + N), M, K, N, "bf16", out, epi)
 
 
+def test_codes_and_inputs_beyond_four_gib():
+    """The last rows lie past 2^32 bytes of X and of the codes; every row against the first ones'."""
+    run_repeated(np.random.default_rng(4), 140000, 31000, 40, "bf16", "bf16")
+
+
 def test_special_values_stay_in_their_token():
     rng = np.random.default_rng(11)
     M, K, N = 70, 400, 150
@@ -494,6 +499,21 @@ def test_helpers_refuse_tensors_of_other_kinds_on_the_gpu():
         qc.qlinear_fp8_t(X, pw, workspace=torch.zeros(256, dtype=torch.uint8, device="cuda"))
     with pytest.raises(qc.QcError):
         qc.qlinear_fp8_t(torch.zeros(0, 16, device="cuda"), pw)
+
+
+def test_a_weight_that_is_not_what_it_says_is_refused():
+    """Its blob too short for its sizes, or its scales."""
+    X, pw = torch.zeros(4, 128, device="cuda"), qc.pack_weight_fp8_t(torch.zeros(128, 128, device="cuda"))
+    off = torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda")
+    for bad in (qc.PackedWeightFp8(pw.blob[:-1], pw.scale, 1, 128, 128), qc.PackedWeightFp8(pw.blob, torch.zeros(1, 2, 1, device="cuda"), 1, 256, 128),
+                qc.PackedWeightFp8(pw.blob, pw.scale, 1, 129, 128)):
+        for helper in (qc.qlinear_fp8_t, qc._python_helpers.get("qlinear_fp8_t", qc.qlinear_fp8_t)):
+            with pytest.raises(ValueError, match="blob|scale"):
+                helper(X, bad, workspace=qc.qlinear_fp8_workspace_t(4, 128, bad.N), Y=torch.zeros(4, bad.N, dtype=torch.bfloat16, device="cuda"))
+        with pytest.raises(ValueError, match="blob|scale"):
+            qc.unpack_weight_codes_fp8_t(bad)
+    with pytest.raises(ValueError, match="blob"):
+        qc.qlinear_fp8_grouped_t(X, qc.PackedWeightFp8(pw.blob, torch.zeros(2, 1, 1, device="cuda"), 2, 128, 128), off)
 
 
 def test_native_helpers_are_the_python_ones():
