@@ -40,9 +40,10 @@ __host__ __device__ inline int64_t fp8_weight_offset(int64_t n, int64_t k, int64
 // bytes of one expert's codes
 __host__ inline int64_t fp8_weight_bytes(int64_t N, int64_t K) { return round_up(N, kTileN) * fp8_blocks(K) * kFp8Block; }
 
-// A tile of the grouped GEMM's tokens: rows [row0, row0 + rows) of X and Y, of one expert; expert < 0: none
+// A tile of the grouped GEMM's tokens: rows [row0, row0 + rows) of X and Y, of one expert; expert < 0: none.  Those that are any
+// come first, `live` of them, in every entry.
 struct Fp8Tile {
-    int32_t row0, rows, expert, pad;
+    int32_t row0, rows, expert, live;
 };
 constexpr int kFp8TokensLeast = 64;   // of the lowest tile a map is made for
 

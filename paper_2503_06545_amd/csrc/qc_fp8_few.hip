@@ -135,10 +135,11 @@ __global__ __launch_bounds__((64 * kWavesMost<SRC, MI, NF>)) void fp8_few_kernel
     const Fp8GemmArgs &g = a.g;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int c = lane & 15, h = lane >> 4;
-    // block b runs on XCD b % 8: the blocks of one XCD take consecutive tiles, token tile fastest, so that they share weights in its L2
-    const int nb = gridDim.x, b = blockIdx.x;
+    // block b runs on XCD b % 8: the blocks of one XCD take consecutive tiles, token tile fastest, so that they share weights in its L2;
+    // grouped they hardly share any, and the tiles without rows, the last ones, come last
+    const int nb = gridDim.x, b = blockIdx.x, channel_tiles = g.n_tiles * (8 / NF);
     const int v = (b % 8) * (nb / 8) + min(b % 8, nb % 8) + b / 8;
-    const int mt = v % g.m_tiles, nt = v / g.m_tiles;
+    const int mt = a.offsets ? b / channel_tiles : v % g.m_tiles, nt = a.offsets ? b % channel_tiles : v / g.m_tiles;
     const int G = nt / (8 / NF), t0 = nt % (8 / NF) * NF;
     if ((int64_t)G * kTileN + t0 >= g.N) return;   // no live channel
     Where at;

@@ -59,7 +59,13 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, h = lane >> 4;
     int v, nt;
-    tile_of_block(blockIdx.x, gridDim.x, a.m_tiles, a.n_tiles, a.group_m, v, nt);
+    int blocks = gridDim.x, m_tiles = a.m_tiles;
+    if (a.map) {   // the tiles that have rows over all XCDs, blocks without one behind them
+        m_tiles = a.map[0].live;
+        blocks = m_tiles * a.n_tiles;
+        if ((int)blockIdx.x >= blocks) return;
+    }
+    tile_of_block(blockIdx.x, blocks, m_tiles, a.n_tiles, a.group_m, v, nt);
     const Where at = tile_of(a, v, TM);
     if (at.expert < 0) return;
     const int first = wave * (16 * MI), live = at.rows - first;   // rows of this wavefront that are stored: may be none

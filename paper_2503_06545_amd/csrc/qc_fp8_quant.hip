@@ -78,7 +78,7 @@ __device__ void make_map(const QuantArgs &a) {
     __syncthreads();
     const int total = first[E];
     for (int v = threadIdx.x; v < a.map_entries; v += kThreads) {
-        Fp8Tile t{0, 0, -1, 0};
+        Fp8Tile t{0, 0, -1, total};
         if (v < total) {
             int e = 0, end = E;   // the last expert that begins at or before v: the one with rows
             while (end - e > 1) {
