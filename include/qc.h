@@ -318,7 +318,7 @@ qc_status qc_qlinear_fp8_grouped(const void *X, qc_dtype xdt, int64_t M, int64_t
                                  int64_t experts, const void *packed, const float *w_scale, int64_t N, const float *bias,
                                  qc_epilogue epi, void *Y, qc_out ydt, void *workspace, size_t workspace_bytes,
                                  void *stream);
-/* Test hook, host only: what a linear does, experts = 0, or a grouped one, its outputs not lying over its inputs.  Returns 0
+/* Test hook, host only: what a linear of bf16 inputs does, experts = 0, or a grouped one, outputs not over inputs.  Returns 0
  * and fills plan[0 .. 3] (host memory); -1 for what the linear refuses and for bad arguments.
  *   0  the kernel of the products: 1 the one that streams weights through a ring in LDS, 3 the one for few tokens
  *   1  tokens of a tile

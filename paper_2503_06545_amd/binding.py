@@ -424,7 +424,7 @@ def qc_debug_linear_plan_fp8(M, K, N, experts, ydt, plan) -> int:
 
 
 def linear_plan_fp8(M: int, K: int, N: int, out: str = "bf16", experts: int = 0) -> dict:
-    """What an 8-bit floating-point linear's launches are (host only): kernel "ring" or "few", tokens and channels of its tiles,
+    """What an 8-bit floating-point linear's launches are for bf16 inputs (host only): kernel "ring" or "few", tokens and channels of its tiles,
     and whether the quantization is fused; experts: of a grouped one."""
     plan = (ctypes.c_int32 * 4)()
     if qc_debug_linear_plan_fp8(M, K, N, experts, OUT[out], ctypes.cast(plan, ctypes.c_void_p)) != 0:

@@ -73,6 +73,8 @@ __host__ inline Fp8Workspace fp8_workspace(int64_t M, int64_t K) {
     return w;
 }
 
+constexpr int kCus = 256;   // of the chip
+
 // ---- launchers ----------------------------------------------------------------------------
 
 // Codes row major with scales [M, KB] (qx), or in the GEMM's order with scales [KB, Mp] (qx_tiled).  offsets: of a grouped
@@ -96,7 +98,7 @@ struct Fp8GemmArgs {
     int KB, m_tiles, n_tiles, group_m;
 };
 
-// The kernels for few tokens (qc_fp8_few.hip): 16, 32 or 64 tokens by 16 times 1, 2 or 4 channels
+// The kernel for few tokens (qc_fp8_few.hip): 16 tokens by 16 times 1, 2 or 4 channels, or 32 by 64
 struct Fp8FewTile {
     int tokens, frags;   // tokens 0: not for these sizes
 };
@@ -106,8 +108,8 @@ struct Fp8Plan {
     Fp8FewTile few;
     int tokens;       // of the tiles, whatever the kernel
 };
-Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, int experts, bool grouped, qc_out ydt, bool may_fuse);
-// X null: from the codes and scales that args names, without offsets
+Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, qc_dtype xdt, int experts, bool grouped, qc_out ydt, bool may_fuse);
+// X null: from the codes and scales that args names
 hipError_t launch_fp8_few(const void *X, qc_dtype xdt, int64_t K, const int32_t *offsets, int experts, const Fp8GemmArgs &args,
                           Fp8FewTile tile, qc_epilogue epi, qc_out ydt, hipStream_t stream);
 

@@ -82,7 +82,7 @@ qc_status gemm(const Fp8GemmArgs &a, int64_t K, const int32_t *offsets, int64_t 
 qc_status linear(const void *X, qc_dtype xdt, int64_t M, int64_t K, const int32_t *offsets, int64_t experts, const void *packed,
                  const float *w_scale, int64_t N, const float *bias, qc_epilogue epi, void *Y, qc_out ydt, void *workspace, void *stream) {
     const size_t x_bytes = (size_t)M * (size_t)K * (xdt == QC_BF16 ? 2 : 4), y_bytes = (size_t)M * (size_t)N * (ydt == QC_OUT_BF16 ? 2 : 4);
-    const Fp8Plan plan = fp8_plan(M, N, K, (int)experts, offsets != nullptr, ydt, !overlap(X, x_bytes, Y, y_bytes));
+    const Fp8Plan plan = fp8_plan(M, N, K, xdt, (int)experts, offsets != nullptr, ydt, !overlap(X, x_bytes, Y, y_bytes));
     const Fp8GemmArgs a = gemm_args(workspace, M, K, packed, w_scale, N, bias, Y, plan, experts, offsets != nullptr);
     if (plan.fused) return device_status(launch_fp8_few(X, xdt, K, offsets, (int)experts, a, plan.few, epi, ydt, (hipStream_t)stream));
     QC_TRY(device_status(launch_fp8_quant(X, xdt, M, K, nullptr, a.x_tiled, a.x_scale, offsets, (int)experts, plan.tokens, a.map, (hipStream_t)stream)));
@@ -143,7 +143,7 @@ extern "C" qc_status qc_qlinear_fp8_gemm(const void *workspace, size_t workspace
     QC_TRY(check_workspace(workspace));
     QC_TRY(check_gemm_supported(M, K, N, 1, ydt));
     if (workspace_bytes < fp8_workspace(M, K).total_bytes) return QC_ERR_WORKSPACE;
-    const Fp8Plan plan = fp8_plan(M, N, K, 1, false, ydt, false);
+    const Fp8Plan plan = fp8_plan(M, N, K, QC_F32, 1, false, ydt, false);
     return gemm(gemm_args(const_cast<void *>(workspace), M, K, packed, w_scale, N, bias, Y, plan, 1, false), K, nullptr, 1, plan, epi, ydt, stream);
 }
 
@@ -178,7 +178,7 @@ extern "C" int qc_debug_linear_plan_fp8(int64_t M, int64_t K, int64_t N, int64_t
     if (M < 1 || K < 1 || N < 1 || experts < 0 || !plan || (ydt != QC_OUT_F32 && ydt != QC_OUT_BF16)) return -1;
     const int64_t matrices = experts ? experts : 1;
     if (check_quant_supported(M, K) != QC_OK || check_gemm_supported(M, K, N, matrices, ydt) != QC_OK) return -1;
-    const Fp8Plan p = fp8_plan(M, N, K, (int)matrices, experts != 0, ydt, true);
+    const Fp8Plan p = fp8_plan(M, N, K, QC_BF16, (int)matrices, experts != 0, ydt, true);
     plan[0] = p.few.tokens ? kGemmSmall : kGemmRing;
     plan[1] = p.tokens;
     plan[2] = p.few.tokens ? kFragRows * p.few.frags : kTileN;

@@ -60,7 +60,8 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
     const int c = lane & 15, h = lane >> 4;
     int v, nt;
     int blocks = gridDim.x, m_tiles = a.m_tiles;
-    if (a.map) {   // the tiles that have rows over all XCDs, blocks without one behind them
+    if (a.map) {   // The tiles that have rows over all XCDs, blocks without one behind them: dealt out together, they left the last XCD the
+                   // empty end (us: 65536 x 4608 x 1152, 64 experts 534, now 514; 3001 x 1000 x 1301, 12 experts 24.3 20.7)
         m_tiles = a.map[0].live;
         blocks = m_tiles * a.n_tiles;
         if ((int)blockIdx.x >= blocks) return;
@@ -315,8 +316,6 @@ hipError_t launch_tiles(const Fp8GemmArgs &a, qc_epilogue epi, hipStream_t strea
 
 }  // namespace
 
-constexpr int kCus = 256;
-
 // What a CU takes for a step of `per_cu` of the ring kernel's tiles of 64 h tokens, in hundredths of a microsecond, read off
 // linears of 300 to 60000 tokens at every height; by it a call takes 1.8 % longer than at its best one, at 128 tokens always 3.5 %, at
 // 192 6.6 %.  A tile that a CU has to itself waits out its own loads, which a lower one has fewer of; from two or three on the
@@ -351,29 +350,39 @@ static int ring_tokens(int64_t M, int64_t N, int experts, bool grouped, bool exa
     return 64 * best;
 }
 
-// The few-token kernel, from X in one launch while its tiles of 16 tokens x 64 channels are at most two to a CU, with fewer
-// channels where that gives at most one (us at 16, 32 and 64 channels: 1 x 1152 x 6912 6.7 4.6 5.0, 1 x 4608 x 1152 7.6 8.0 8.8, 64 x 1152
-// x 1152 7.3 4.9 5.6, 162 rows of 52 experts, 1152 x 44, 8.5 5.8 6.2; the ring 12.5 29.6 12.6 10.8).  A long reduction casts more in
-// each block than more than 64 tokens are worth, a very long one at all (137 rows of 3 experts, 3909 x 1187, 18.1, from codes 13.6; 47 x
-// 6813 x 89 20.8 14.4).  From codes with tiles of 32 x 64 while these are at most one to a CU (300 x 4608 x 1152 13.5, ring of 64
-// tokens 20.2; binary32 17.0 34.7), with a long reduction two for binary32 outputs (600 x 4608 x 1152 28 36).
-Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, int experts, bool grouped, qc_out ydt, bool may_fuse) {
+// The few-token kernel while its tiles are few, read off 17000 drawn calls of 4 to 700 tokens with one weight and with up to 100
+// experts, at every tile and both counts of wavefronts: by it a call takes 2.0 % longer than at its best one.
+//
+// From X in one launch, tiles of 16 tokens by as few channels as give a CU one at most (us at 16, 32 and 64 channels: 1 x 1152 x 6912 6.7 4.6
+// 5.0, 1 x 4608 x 1152 7.6 8.0 8.8, 64 x 1152 x 1152 7.3 4.9 5.6).  Every channel tile casts the same tokens again, so a long
+// reduction had better be cast once (tiles of 64 channels up to 24 blocks of 128, others up to 36), and so had bf16 rows that begin at
+// odd elements, whose loads are split (16 x 3951 x 3456 14.5, from codes 9.6).  Beyond one tile to a CU short reductions
+// gain by it up to two (33 x 577 x 9113 7.4, ring 8.1), and a few rows of many experts, whose tiles are mostly of one row and
+// whose upper bound is half empty, up to eight (32 x 2048 x 1408, 64 experts 15.7, ring 17.1; 16 x 1152 x 4608, 32 experts 14.5 15.8).
+//
+// From codes tiles of 32 x 64 while these are one to a CU (300 x 4608 x 1152 13.5, ring of 64 tokens 20.2; binary32 17.0 34.7), with
+// a reduction longer than nine blocks two (200 x 4608 x 4608 17.7, ring 18.7; binary32 21.5 31.8).
+Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, qc_dtype xdt, int experts, bool grouped, qc_out ydt, bool may_fuse) {
     Fp8Plan p{};
-    const bool exact = ydt == QC_OUT_F32, lengthy = fp8_blocks(K) >= 18;
-    const int64_t most = 2 * kCus * 8 * kTileN;   // beyond this the tile counts below need not be made
+    const int64_t KB = fp8_blocks(K), most = 8 * kCus * 8 * kTileN;   // beyond this the tile counts below need not be made
     if (M <= most && N <= most) {
+        const bool odd = xdt == QC_BF16 && K % 2, rows_few = grouped && M <= 96;
         auto tiles = [&](int tokens, int frags) {
             const int64_t m = grouped ? fp8_tiles_most(M, experts, tokens) : (M + tokens - 1) / tokens;
             return m * (round_up(N, kTileN) / kTileN) * (8 / frags);   // a tile's channels lie eight apart: any N has all of a group's
         };
-        if (may_fuse && tiles(16, 4) <= 2 * kCus && M <= (lengthy ? 64 : 512) && fp8_blocks(K) <= 36) {
-            p.fused = true;
-            p.few = {16, tiles(16, 1) <= kCus / 2 ? 1 : tiles(16, 2) <= kCus ? 2 : 4};
-        } else if (tiles(32, 4) <= (exact && lengthy ? 2 : 1) * kCus) {
-            p.few = {32, 4};
+        int frags = 0;
+        if (may_fuse && KB <= (odd ? 17 : 36)) {
+            if (tiles(16, 1) <= kCus) frags = 1;
+            else if (tiles(16, 2) <= kCus) frags = 2;
+            else if (tiles(16, 4) <= kCus && (rows_few || KB <= 24)) frags = 4;
+            else if (tiles(16, 4) <= (rows_few ? 8 : 2) * kCus && KB <= (odd ? 5 : rows_few ? 36 : 9)) frags = 4;
         }
+        p.fused = frags != 0;
+        if (p.fused) p.few = {16, frags};
+        else if (tiles(32, 4) <= (KB <= 9 ? 1 : rows_few ? 4 : 2) * kCus) p.few = {32, 4};
     }
-    p.tokens = p.few.tokens ? p.few.tokens : ring_tokens(M, N, experts, grouped, exact);
+    p.tokens = p.few.tokens ? p.few.tokens : ring_tokens(M, N, experts, grouped, ydt == QC_OUT_F32);
     return p;
 }
 

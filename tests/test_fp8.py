@@ -151,7 +151,9 @@ def test_plans():
     assert plan(1, 1152, 6912) == {"kernel": "few", "tokens": 16, "channels": 32, "fused": True}
     assert plan(1, 4608, 1152)["channels"] == 16 and plan(130, 1152, 1152)["channels"] == 64
     assert plan(300, 4608, 1152) == {"kernel": "few", "tokens": 32, "channels": 64, "fused": False}
-    assert plan(600, 4608, 1152, "f32")["kernel"] == "few" and plan(600, 4608, 1152)["kernel"] == "ring"
+    assert plan(600, 4608, 1152, "f32")["kernel"] == plan(600, 4608, 1152)["kernel"] == "few" and plan(1200, 4608, 1152)["kernel"] == "ring"
+    assert plan(100, 1152, 9000)["kernel"] == "ring" and plan(16, 1152, 4608, experts=32) == {"kernel": "few", "tokens": 16, "channels": 64, "fused": True}
+    assert plan(16, 3951, 3456) == plan(16, 3952, 9000) == {"kernel": "few", "tokens": 32, "channels": 64, "fused": False}
     assert plan(131072, 1152, 4608) == {"kernel": "ring", "tokens": 256, "channels": 128, "fused": False}
     assert plan(131072, 1152, 4608, "f32")["tokens"] == 128 and plan(1200, 1152, 1152)["tokens"] == 64
     assert plan(8, 4608, 1152, experts=32)["fused"] and plan(200, 1152, 4608, experts=32)["tokens"] == 64
