@@ -77,6 +77,10 @@ constexpr int kCus = 256;   // of the chip
 
 // ---- launchers ----------------------------------------------------------------------------
 
+// the quantizer's blocks of threads for each 128 columns, in eights
+constexpr int kFp8QuantRows = 32;
+__host__ inline int64_t fp8_quant_row_blocks(int64_t M) { return round_up((M + kFp8QuantRows - 1) / kFp8QuantRows, 8); }
+
 // Codes row major with scales [M, KB] (qx), or in the GEMM's order with scales [KB, Mp] (qx_tiled).  offsets: of a grouped
 // linear, device int32 [experts + 1]: rows of no group are passed over, and the map of its tiles of `tokens` rows is made if
 // there is one.

@@ -36,7 +36,7 @@ qc_status check_weight_side(const void *packed, const float *w_scale, const floa
 }
 
 qc_status check_quant_supported(int64_t M, int64_t K) {
-    return K > QC_MAX_K || M > 0x7fffffffLL || (M + 31) / 32 * fp8_blocks(K) >= kBlocksMost ? QC_ERR_UNSUPPORTED : QC_OK;
+    return K > QC_MAX_K || M > 0x7fffffffLL || fp8_quant_row_blocks(M) * fp8_blocks(K) >= kBlocksMost ? QC_ERR_UNSUPPORTED : QC_OK;
 }
 
 qc_status check_gemm_supported(int64_t M, int64_t K, int64_t N, int64_t experts, qc_out ydt) {

@@ -14,6 +14,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kRowsPerWave = 8;   // eight lanes each
+static_assert(kWaves * kRowsPerWave == kFp8QuantRows);
 
 // eight lanes' share of columns col0 .. col0 + 127 of a row of K at any alignment, zeros past its end
 template <bool NT, typename XT>
@@ -96,7 +97,9 @@ __device__ void make_map(const QuantArgs &a) {
 
 // A wavefront takes eight rows x one block of 128 columns: the shorter its chain, the shorter a small call, and the more of
 // them there are on the large ones (us at one and three blocks: 16 x 4608 2.6 3.7, 300 x 4608 binary32 4.0 6.6, 16384 x 1152 13.6
-// 16.1, 131072 x 1152 80 89, 65536 x 4608 161 169).  NT: see stream_loads().
+// 16.1, 131072 x 1152 80 89, 65536 x 4608 161 169).  Block i runs on XCD i % 8, which takes a row's blocks of columns one after
+// another, so that lines that two of them share, of X or of the codes, meet in its L2 (200000 x 1000 267, now 144; 65536 x 4608 167
+// 155).  NT: see stream_loads().
 template <typename XT, bool NT>
 __global__ __launch_bounds__(kThreads) void fp8_quant_kernel(QuantArgs a) {
     if (a.map && (int)blockIdx.x == a.quant_blocks) {
@@ -105,8 +108,9 @@ __global__ __launch_bounds__(kThreads) void fp8_quant_kernel(QuantArgs a) {
     }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int sub = lane & 7;
-    const int64_t row_block = blockIdx.x / (uint32_t)a.KB;
-    const int b = blockIdx.x % (uint32_t)a.KB;
+    const uint32_t of_eight = blockIdx.x % (8u * a.KB);
+    const int64_t row_block = blockIdx.x / (8u * a.KB) * 8 + of_eight % 8;
+    const int b = of_eight / 8;
     const int64_t row = (row_block * kWaves + wave) * kRowsPerWave + lane / 8;
     if (row >= a.M) return;
     if (a.offsets && (row < a.offsets[0] || row >= a.offsets[a.experts])) return;   // of no group
@@ -144,10 +148,11 @@ __global__ __launch_bounds__(kThreads) void fp8_quant_kernel(QuantArgs a) {
 // X past the caches: it is not read again, and what it would push out of the last-level cache are codes that the products are
 // about to read, from some 32 MB of it on (us, ordinary and non-temporal loads, four inputs in turn: 32 MB 13.6 12.7, binary32
 // 22.0 20.0, 604 MB 161 157; but 4 MB binary32 3.9 4.2).  Codes that stay row by row win from 200 MB of both on (131072 x 1152 82.9 78.5,
-// 65536 x 4608 170 161, 38 MB 12.3 13.6).
-bool stream_loads(int64_t x_bytes, int64_t code_bytes, bool tiled) {
+// 65536 x 4608 170 161, 38 MB 12.3 13.6).  Rows that are no whole lines share some, which it would fetch twice (100000 x 1000
+// 72 79, 60000 x 4600 169 184).
+bool stream_loads(int64_t x_bytes, int64_t code_bytes, bool tiled, bool whole_lines) {
     constexpr int64_t MB = 1 << 20;
-    return tiled ? x_bytes >= 32 * MB : x_bytes + code_bytes >= 200 * MB;
+    return whole_lines && (tiled ? x_bytes >= 32 * MB : x_bytes + code_bytes >= 200 * MB);
 }
 
 // ---- weights ------------------------------------------------------------------------------------
@@ -211,7 +216,7 @@ hipError_t launch_fp8_quant(const void *X, qc_dtype xdt, int64_t M, int64_t K, u
     a.K = K;
     a.Mp = round_up(M, kWaveM);
     a.KB = (int)fp8_blocks(K);
-    a.quant_blocks = (int)((M + kWaves * kRowsPerWave - 1) / (kWaves * kRowsPerWave) * a.KB);
+    a.quant_blocks = (int)(fp8_quant_row_blocks(M) * a.KB);
     a.offsets = offsets;
     a.experts = experts;
     if (map) {
@@ -220,7 +225,8 @@ hipError_t launch_fp8_quant(const void *X, qc_dtype xdt, int64_t M, int64_t K, u
         a.map_entries = (int)fp8_tiles_most(M, experts, tokens);
     }
     const dim3 grid((unsigned)(a.quant_blocks + (map ? 1 : 0))), block(kThreads);
-    const bool nt = stream_loads(M * K * (xdt == QC_BF16 ? 2 : 4), M * K, qx_tiled != nullptr);
+    const int64_t element = xdt == QC_BF16 ? 2 : 4;
+    const bool nt = stream_loads(M * K * element, M * K, qx_tiled != nullptr, K * element % 128 == 0);
     if (xdt == QC_BF16) {
         if (nt) fp8_quant_kernel<uint16_t, true><<<grid, block, 0, stream>>>(a);
         else fp8_quant_kernel<uint16_t, false><<<grid, block, 0, stream>>>(a);
