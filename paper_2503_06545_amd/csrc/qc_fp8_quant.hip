@@ -99,8 +99,8 @@ __device__ void make_map(const QuantArgs &a) {
 // them there are on the large ones (us at one and three blocks: 16 x 4608 2.6 3.7, 300 x 4608 binary32 4.0 6.6, 16384 x 1152 13.6
 // 16.1, 131072 x 1152 80 89, 65536 x 4608 161 169).  Block i runs on XCD i % 8, which takes a row's blocks of columns one after
 // another, so that lines that two of them share, of X or of the codes, meet in its L2 (200000 x 1000 267, now 144; 65536 x 4608 167
-// 155).  NT: see stream_loads().
-template <typename XT, bool NT>
+// 155).  NT, NTS: see streams().
+template <typename XT, bool NT, bool NTS>
 __global__ __launch_bounds__(kThreads) void fp8_quant_kernel(QuantArgs a) {
     if (a.map && (int)blockIdx.x == a.quant_blocks) {
         make_map(a);
@@ -127,32 +127,46 @@ __global__ __launch_bounds__(kThreads) void fp8_quant_kernel(QuantArgs a) {
         w[d] = e4m3x4(quotient(g.get(4 * d + 0), s, r), quotient(g.get(4 * d + 1), s, r), quotient(g.get(4 * d + 2), s, r),
                       quotient(g.get(4 * d + 3), s, r));
     const uint4 out = Group<XT>::gather_codes(w, sub);
+    const u32x4 codes = {out.x, out.y, out.z, out.w};
     const int unit = Group<XT>::unit_of(sub);
     if (a.qx_tiled) {
         const int64_t half = ((row / kWaveM) * a.KB + b) * 8 + (row % kWaveM) / kFragRows * 2 + unit / 4;
-        *reinterpret_cast<uint4 *>(a.qx_tiled + half * kFragBytes + (unit % 4) * 256 + (row % kFragRows) * 16) = out;
+        store_piece<false, !NTS>(reinterpret_cast<u32x4 *>(a.qx_tiled + half * kFragBytes + (unit % 4) * 256 + (row % kFragRows) * 16), codes);
         if (sub == 0) a.x_scale[(int64_t)b * a.Mp + row] = s;
     } else {
         const int64_t col = (int64_t)b * kFp8Block + unit * kUnit;
         uint8_t *const p = a.qx + row * a.K + col;
         if (col + kUnit <= a.K) {
-            __builtin_memcpy(p, &out, sizeof(out));   // at any alignment
+            store_piece<true, !NTS>(reinterpret_cast<u32x4 *>(p), codes);
         } else {
-            const uint32_t v[4] = {out.x, out.y, out.z, out.w};
-            for (int e = 0; e < (int)(a.K - col); ++e) p[e] = (uint8_t)(v[e / 4] >> (8 * (e % 4)));
+            for (int e = 0; e < (int)(a.K - col); ++e) p[e] = (uint8_t)(codes[e / 4] >> (8 * (e % 4)));
         }
         if (sub == 0) a.x_scale[row * a.KB + b] = s;
     }
 }
 
-// X past the caches: it is not read again, and what it would push out of the last-level cache are codes that the products are
-// about to read, from some 32 MB of it on (us, ordinary and non-temporal loads, four inputs in turn: 32 MB 13.6 12.7, binary32
-// 22.0 20.0, 604 MB 161 157; but 4 MB binary32 3.9 4.2).  Codes that stay row by row win from 200 MB of both on (131072 x 1152 82.9 78.5,
-// 65536 x 4608 170 161, 38 MB 12.3 13.6).  Rows that are no whole lines share some, which it would fetch twice (100000 x 1000
-// 72 79, 60000 x 4600 169 184).
-bool stream_loads(int64_t x_bytes, int64_t code_bytes, bool tiled, bool whole_lines) {
+// Which accesses of a call go past the caches.  X: it is not read again, and what it would push out of the last-level cache are codes
+// that the products are about to read, from some 32 MB of it on (us, ordinary and non-temporal loads, four inputs in turn: 32 MB 13.6 12.7,
+// binary32 22.0 20.0, 604 MB 161 157; but 4 MB binary32 3.9 4.2).  Rows that are no whole lines share some, which it would fetch
+// twice (100000 x 1000 72 79, 60000 x 4600 169 184).  Codes for the products only where that cache would not keep them either (the whole
+// linear with 1152 channels: 346 MB of codes 597 582, 604 MB 935 909; but 230 MB 367 390, 302 MB 458 462).  Codes that stay row by row,
+// with X, from 200 MB of both on (16384 x 4608 40.4 39.0, 65536 x 4608 156 146, 131072 x 4608 309 290; X alone at 38 MB 12.3 13.6).
+struct Streams {
+    bool x, codes;
+};
+Streams streams(int64_t M, int64_t K, int64_t element, bool tiled) {
     constexpr int64_t MB = 1 << 20;
-    return whole_lines && (tiled ? x_bytes >= 32 * MB : x_bytes + code_bytes >= 200 * MB);
+    if (K * element % 128) return {false, false};
+    if (tiled) return {M * K * element >= 32 * MB, M * K >= 320 * MB};
+    const bool large = M * K * (element + 1) >= 200 * MB;
+    return {large, large && K % 128 == 0};
+}
+
+template <typename XT>
+void launch_quant(const QuantArgs &a, Streams past, dim3 grid, hipStream_t stream) {
+    if (past.codes) fp8_quant_kernel<XT, true, true><<<grid, kThreads, 0, stream>>>(a);
+    else if (past.x) fp8_quant_kernel<XT, true, false><<<grid, kThreads, 0, stream>>>(a);
+    else fp8_quant_kernel<XT, false, false><<<grid, kThreads, 0, stream>>>(a);
 }
 
 // ---- weights ------------------------------------------------------------------------------------
@@ -224,16 +238,10 @@ hipError_t launch_fp8_quant(const void *X, qc_dtype xdt, int64_t M, int64_t K, u
         a.tokens = tokens;
         a.map_entries = (int)fp8_tiles_most(M, experts, tokens);
     }
-    const dim3 grid((unsigned)(a.quant_blocks + (map ? 1 : 0))), block(kThreads);
-    const int64_t element = xdt == QC_BF16 ? 2 : 4;
-    const bool nt = stream_loads(M * K * element, M * K, qx_tiled != nullptr, K * element % 128 == 0);
-    if (xdt == QC_BF16) {
-        if (nt) fp8_quant_kernel<uint16_t, true><<<grid, block, 0, stream>>>(a);
-        else fp8_quant_kernel<uint16_t, false><<<grid, block, 0, stream>>>(a);
-    } else {
-        if (nt) fp8_quant_kernel<float, true><<<grid, block, 0, stream>>>(a);
-        else fp8_quant_kernel<float, false><<<grid, block, 0, stream>>>(a);
-    }
+    const dim3 grid((unsigned)(a.quant_blocks + (map ? 1 : 0)));
+    const Streams past = streams(M, K, xdt == QC_BF16 ? 2 : 4, qx_tiled != nullptr);
+    if (xdt == QC_BF16) launch_quant<uint16_t>(a, past, grid, stream);
+    else launch_quant<float>(a, past, grid, stream);
     return hipGetLastError();
 }
 

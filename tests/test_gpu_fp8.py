@@ -92,6 +92,21 @@ def test_quant_act_on_values_at_the_borders_of_codes(dtype):
         assert bits_equal(s.cpu().numpy(), s_ref) and np.array_equal(to_codes(q), plain_zeros(q_ref))
 
 
+# past the caches with and without whole lines of codes, through them where X has none; rows 32 to a block, blocks in eights
+@pytest.mark.parametrize("M,K,dtype", [(70003, 1152, "bf16"), (40001, 1152, "f32"), (70003, 1088, "bf16"), (70003, 1001, "bf16"), (50021, 1056, "f32")])
+def test_large_inputs_are_the_small_ones_bit_for_bit(M, K, dtype):
+    """The rows of a small block repeated, the block against the oracle and every row against the block's."""
+    period = 53
+    x = random_x(np.random.default_rng(K), period, K, dtype)
+    q_ref, s_ref = oracle.quant_act_fp8(x)
+    q, s = qc.quant_act_fp8_t(dev(x).repeat(-(-M // period), 1)[:M].contiguous())
+    q = q.view(torch.uint8)
+    assert bits_equal(s[:period].cpu().numpy(), s_ref) and np.array_equal(to_codes(q[:period]), plain_zeros(q_ref))
+    whole = M // period * period
+    for t in (q, s):
+        assert bool((t[:whole].view(-1, period, t.shape[1]) == t[:period]).all()) and torch.equal(t[whole:], t[:M - whole])
+
+
 def test_quant_act_into_given_tensors_writes_nothing_else():
     x = random_x(np.random.default_rng(3), 21, 203, "f32")
     codes = torch.full((21 * 203 + 64,), 0x55, dtype=torch.uint8, device="cuda")
@@ -263,7 +278,8 @@ def run_repeated_groups(rng, sizes, K, N, out="bf16"):
 # the sizes of real layers, sampled
 @pytest.mark.parametrize("M,K,N,out,epi", [(16384, 1152, 3456, "bf16", "none"), (20000, 4608, 1152, "f32", "none"), (9000, 1152, 4608, "bf16", "gelu_tanh"),
                                            (40000, 1152, 4608, "bf16", "gelu_tanh"), (4099, 1000, 1301, "f32", "gelu_erf"),
-                                           (2500, 9216, 640, "bf16", "none"), (700000, 128, 3200, "bf16", "none")])
+                                           (2500, 9216, 640, "bf16", "none"), (700000, 128, 3200, "bf16", "none"),
+                                           (300007, 1152, 20, "bf16", "none")])
 def test_large_linears(M, K, N, out, epi):
     run_repeated(np.random.default_rng(M + N), M, K, N, "bf16", out, epi)
 
