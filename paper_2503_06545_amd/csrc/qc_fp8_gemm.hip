@@ -4,6 +4,8 @@
 //
 // One v_mfma_f32_16x16x128_f8f6f4 covers a block, so P_b comes out of the matrix unit with nothing to add it to, and the
 // scales are one fma per output and block on the vector unit, half as many issue cycles as the matrix instruction's.
+#include <math.h>
+
 #include "qc_fp8_device.h"
 
 namespace qc {
@@ -316,22 +318,26 @@ hipError_t launch_tiles(const Fp8GemmArgs &a, qc_epilogue epi, hipStream_t strea
 
 }  // namespace
 
-// What a CU takes for a step of `per_cu` of the ring kernel's tiles of 64 h tokens, in hundredths of a microsecond, read off
-// linears of 300 to 60000 tokens at every height; by it a call takes 1.8 % longer than at its best one, at 128 tokens always 3.5 %, at
-// 192 6.6 %.  A tile that a CU has to itself waits out its own loads, which a lower one has fewer of; from two or three on the
-// products count, and for binary32 outputs their widening; and on calls that go on for long, where power does, what a
-// higher tile moves less for each product.  (us at 256 / 192 / 128 / 64 tokens: 300 x 4608 x 1152 - 31.3 25.2 20.2, 5000 x 1152 x 4608 -
-// 41.5 39.8 47.0, 33199 x 1152 x 4608 203 199 203 264, 65536 x 4608 x 1152 450 462 481; binary32, 128 / 64: 300 x 4608 x 1152
-// 46.0 34.7, 4099 x 1000 x 1301 31.3 28.8, 10000 x 1152 x 4608 132 144.)
-static double step_cost(int h, double per_cu, bool exact) {
+// What a CU takes for its share of the ring kernel's tiles of 64 h tokens, `per_cu` of them, in microseconds, with `exact` in hundredths of one for
+// each step: read off 3000 drawn linears of 1500 to 60000 tokens, half with 2 to 64 experts, at every height; by it a call takes 0.7 % longer than at
+// its best one, at 128 tokens always 3.8 %, at 192 7.2 %.  A step costs a tile the less for each token the higher it is; a CU that has one
+// tile or two waits out loads, which a lower one has fewer of; and higher tiles leave more of the last round idle.
+// (us at 256 / 192 / 128 / 64 tokens: 300 x 4608 x 1152 - 31.3 25.2 20.2, 5000 x 1152 x 4608 - 41.5 39.8 47.0, 65536 x 4608 x 1152 439 450 464,
+// 131072 x 1152 x 4608 739 754 784, 32768 x 1152 x 4608 of 16 experts 211 202 214; binary32, 128 / 64, where the products' widening counts: 300 x 4608 x 1152 46.0 34.7, 4099 x 1000 x 1301
+// 31.3 28.8, 10000 x 1152 x 4608 132 144.)
+static double ring_cost(int h, double per_cu, int64_t KB, bool grouped, bool exact) {
     if (exact) return h == 1 ? (per_cu <= 1 ? 85 : per_cu <= 2 ? 140 : 68 * per_cu) : per_cu <= 1 ? 115 : per_cu <= 2 ? 210 : 120 * per_cu;
-    if (h == 1) return per_cu <= 1 ? 45 : per_cu <= 2 ? 69 : 42 * per_cu;
-    if (h == 2) return per_cu <= 1 ? 60 : per_cu <= 2 ? 95 : 60 * per_cu;
-    if (h == 3) return per_cu <= 1 ? 85 : 84 * per_cu;
-    return per_cu <= 1 ? 108 : (per_cu < 12 ? 122 : 110) * per_cu;
+    static const struct {
+        double step, tile, last, one, two;   // a step, the rest of a tile, what the last round is short of; one or two tiles to a CU
+    } kHeight[] = {{0.36, 0.46, 0.10, 0.12, 1.74}, {0.48, 0.81, 0.07, 1.28, 1.39}, {0.60, 1.53, 0.33, 1.02, 1.58}, {0.76, 2.21, 0.62, 1.60, 2.30}};
+    const auto &k = kHeight[h - 1];
+    const double t = (double)KB * k.step + k.tile;
+    if (per_cu <= 1) return k.one * t;   // nothing is lower than one of the lowest tiles
+    if (per_cu <= 2) return k.two * t;
+    return (!grouped && per_cu <= 4 ? ceil(per_cu) : per_cu + k.last) * t;
 }
 
-static int ring_tokens(int64_t M, int64_t N, int experts, bool grouped, bool exact) {
+static int ring_tokens(int64_t M, int64_t N, int64_t K, int experts, bool grouped, bool exact) {
     const int64_t n_tiles = round_up(N, kTileN) / kTileN;
     int best = 0;
     double least = 0;
@@ -342,9 +348,9 @@ static int ring_tokens(int64_t M, int64_t N, int experts, bool grouped, bool exa
             per_cu = live * (each > 1 ? each : 1) * (double)n_tiles / kCus;
         } else {
             const int64_t tiles = (M + 64 * h - 1) / (64 * h) * n_tiles;
-            per_cu = tiles <= 4 * kCus ? (double)((tiles + kCus - 1) / kCus) : (double)tiles / kCus;
+            per_cu = exact && tiles <= 4 * kCus ? (double)((tiles + kCus - 1) / kCus) : (double)tiles / kCus;
         }
-        const double cost = step_cost(h, per_cu, exact);
+        const double cost = ring_cost(h, per_cu, fp8_blocks(K), grouped, exact);
         if (best == 0 || cost < least) { best = h; least = cost; }
     }
     return 64 * best;
@@ -382,7 +388,7 @@ Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, qc_dtype xdt, int experts, boo
         if (p.fused) p.few = {16, frags};
         else if (tiles(32, 4) <= (KB <= 9 ? 1 : rows_few ? 4 : 2) * kCus) p.few = {32, 4};
     }
-    p.tokens = p.few.tokens ? p.few.tokens : ring_tokens(M, N, experts, grouped, ydt == QC_OUT_F32);
+    p.tokens = p.few.tokens ? p.few.tokens : ring_tokens(M, N, K, experts, grouped, ydt == QC_OUT_F32);
     return p;
 }
 

@@ -196,7 +196,7 @@ def which(M, K, N, out, experts=0):
 # (kernel, tokens, channels, fused), a ragged reduction and channels, and whether the output may be binary32
 KERNELS = [(("few", 16, 16, True), 700, 700, 2), (("few", 16, 32, True), 1153, 2311, 2), (("few", 16, 64, True), 513, 4609, 2),
            (("few", 32, 64, False), 5001, 700, 2), (("ring", 64, 128, False), 260, 1300, 2), (("ring", 128, 128, False), 130, 1301, 2),
-           (("ring", 192, 128, False), 257, 701, 1), (("ring", 256, 128, False), 385, 6901, 1)]
+           (("ring", 192, 128, False), 257, 701, 1), (("ring", 256, 128, False), 1281, 6901, 1)]
 
 
 def tokens_for(kernel, K, N, out, experts=0):
@@ -238,10 +238,12 @@ def test_every_kernel_grouped(kernel, out):
 
 @pytest.mark.parametrize("blocks", range(1, 14))
 def test_every_length_of_the_rings_last_steps(blocks):
-    """Six steps to a turn of the ring, and what is left of one."""
+    """Six steps to a turn of the ring, and what is left of one.  Tiles of 256 tokens are for four blocks and more."""
     K = 128 * blocks - blocks % 3
     for what, out in ((("ring", 64, 128, False), "f32"), (("ring", 128, 128, False), "bf16"), (("ring", 192, 128, False), "bf16"), (("ring", 256, 128, False), "bf16")):
         N = 6901 if what[1] == 256 else 301
+        if what[1] == 256 and blocks < 4:
+            continue
         run_repeated(np.random.default_rng(blocks), tokens_for(what, K, N, out), K, N, "bf16", out)
 
 
