@@ -56,3 +56,74 @@ def test_disordered_offsets_reach_nothing_outside(what, K, N, out):
         assert (space[:4096] == 0x5a).all() and (space[4096 + nbytes:] == 0x5a).all(), offsets
     if not what[3]:   # in two launches the workspace is what they meet in
         assert (space[4096:4096 + nbytes] != 0x5a).any()
+
+
+# ---- special values ------------------------------------------------------------------------------
+
+def edge_rows(tokens, M):
+    """First and last row, and both sides of the tiles' edges; others are left."""
+    rows = sorted({m for m in (0, 15, 16, tokens - 1, tokens, 2 * tokens, M - 1) if 0 <= m < M})
+    return rows if len(rows) < M else [0, M - 1]
+
+
+def spoil(X, rows, first):
+    """A NaN or an infinity in each of these rows, in the first and the last column and between."""
+    K = X.shape[1]
+    for i, m in enumerate(rows):
+        X[m, (0, K - 1, K // 2)[(i + first) % 3]] = (float("nan"), float("inf"), -float("inf"))[i % 3]
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("grouped", [False, True])
+@pytest.mark.parametrize("what,K,N,out", EVERY)
+def test_special_values_make_their_tokens_nan_and_no_others(what, K, N, out, grouped, x):
+    E = 3 if grouped else 0
+    M = rows_for(what, K, N, out, E)
+    assert which(M, K, N, out, E) == what
+    g = generator(M + K)
+    pw = random_weight(g, max(E, 1), N, K)
+    X = torch.randn(M, K, generator=g, device="cuda").to(DTYPE[x])
+    bias = torch.randn(*([E] if E else []), N, generator=g, device="cuda")
+    if grouped:   # one row on either side is of no group
+        cut = [1, 1 + (M - 2) // 3, 1 + (M - 2) // 3, M - 1]
+        off = torch.tensor(cut, dtype=torch.int32, device="cuda")
+
+    def run(X):
+        Y = torch.full((M, N), 7.0, dtype=DTYPE[out], device="cuda")
+        if grouped:
+            return qc.qlinear_fp8_grouped_t(X, pw, off, bias, "gelu_tanh", out, Y=Y)
+        return qc.qlinear_fp8_t(X, pw, bias, "gelu_erf", out, Y=Y)
+
+    clean = run(X)
+    assert torch.isfinite(clean).all()
+    for first in range(3):
+        spoilt = X.clone()
+        rows = edge_rows(what[1], M)
+        if grouped:   # also the last and the first row of two groups that meet
+            rows = sorted({*rows, cut[1] - 1, cut[2]} if M > 8 else {0, 1, M - 1})
+        spoil(spoilt, rows, first)
+        y = run(spoilt)
+        mine = [m for m in rows if not grouped or cut[0] <= m < cut[-1]]
+        others = torch.ones(M, dtype=torch.bool, device="cuda")
+        others[mine] = False
+        assert others.any() and (not mine or torch.isnan(y[mine]).all()), first
+        assert torch.equal(y[others], clean[others]), first
+
+
+@pytest.mark.parametrize("what,K,N,out", EVERY)
+def test_zero_rows_and_a_zero_matrix_give_the_bias_in_every_kernel(what, K, N, out):
+    M = rows_for(what, K, N, out)
+    assert which(M, K, N, out) == what
+    g = generator(M + N)
+    bias = torch.randn(N, generator=g, device="cuda")
+    want = bias.to(DTYPE[out])
+    X = torch.randn(M, K, generator=g, device="cuda").bfloat16()
+    zero = qc.pack_weight_fp8_t(torch.zeros(N, K, device="cuda"))
+    assert (qc.qlinear_fp8_t(X, zero, bias, out=out) == want).all()
+    rows = edge_rows(what[1], M)
+    X[rows] = 0.0
+    y = qc.qlinear_fp8_t(X, random_weight(g, 1, N, K), bias, out=out)
+    assert (y[rows] == want).all() and len(rows) < M
+    others = torch.ones(M, dtype=torch.bool, device="cuda")
+    others[rows] = False
+    assert (y[others] != want).any(dim=1).all()
