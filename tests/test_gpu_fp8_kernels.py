@@ -9,6 +9,7 @@ from test_gpu_fp8 import KERNELS, which
 
 pytestmark = pytest.mark.gpu
 
+ONE_LAUNCH, RING = [k for k in KERNELS if k[0][3]], [k for k in KERNELS if k[0][0] == "ring"]
 DTYPE = {"f32": torch.float32, "bf16": torch.bfloat16}
 # every kernel with every output that it is for: ((kernel, tokens, channels, fused), K, N, output)
 EVERY = [(what, K, N, out) for what, K, N, outs in KERNELS for out in ("bf16", "f32")[:outs]]
@@ -127,3 +128,149 @@ def test_zero_rows_and_a_zero_matrix_give_the_bias_in_every_kernel(what, K, N, o
     others = torch.ones(M, dtype=torch.bool, device="cuda")
     others[rows] = False
     assert (y[others] != want).any(dim=1).all()
+
+
+# ---- the calls of a program, through every kernel --------------------------------------------------
+
+@pytest.mark.parametrize("what,K,N,out", EVERY)
+def test_captured_and_replayed_through_every_kernel(what, K, N, out):
+    """A linear and a grouped one that share a workspace; inputs and group sizes change between the replays."""
+    E = 3
+    M, G = rows_for(what, K, N, out), rows_for(what, K, N, out, E)
+    assert which(M, K, N, out) == which(G, K, N, out, E) == what
+    g = generator(M + 1)
+    one, pw = random_weight(g, 1, N, K), random_weight(g, E, N, K)
+    X = torch.randn(max(M, G), K, generator=g, device="cuda").bfloat16()
+    off = torch.tensor([0, G // 3, G // 3, G], dtype=torch.int32, device="cuda")
+    ws = qc.qlinear_fp8_workspace_t(max(M, G), K, N)
+    Y, Z = torch.empty(M, N, dtype=DTYPE[out], device="cuda"), torch.empty(G, N, dtype=DTYPE[out], device="cuda")
+
+    def step():
+        qc.qlinear_fp8_t(X[:M], one, None, "none", out, ws, Y)
+        qc.qlinear_fp8_grouped_t(X[:G], pw, off, None, "none", out, ws, Z)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    rng = np.random.default_rng(M)
+    for turn in range(4):
+        X.copy_(torch.randn(X.shape, generator=g, device="cuda"))
+        cut = sorted(int(v) for v in rng.integers(0, G + 1, size=E + 1))   # rows of no group on both sides
+        off.copy_(torch.tensor(cut, dtype=torch.int32))
+        for t in (Y, Z):
+            t.fill_(3.0)
+        step()
+        torch.cuda.synchronize()
+        want = Y.clone(), Z.clone()
+        for t in (Y, Z):
+            t.fill_(3.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(Y, want[0]) and torch.equal(Z, want[1]), turn
+        assert (Z[:cut[0]] == 3.0).all() and (Z[cut[-1]:] == 3.0).all(), turn
+        assert not (Y == 3.0).all(dim=1).any(), turn
+
+
+@pytest.mark.parametrize("what,K,N,outs", RING)
+def test_halves_on_the_ring(what, K, N, outs):
+    """One input, quantized once, through two linears, the first of them twice: the bits of the whole calls, which take the
+    same launches."""
+    out = ("bf16", "f32")[outs - 1]
+    M = rows_for(what, K, N, out)
+    assert which(M, K, N, out) == what and not what[3]
+    g = generator(N)
+    weights = [random_weight(g, 1, n, K) for n in (N, N + 3)]
+    assert which(M, K, N + 3, out) == what
+    X = torch.randn(M, K, generator=g, device="cuda").bfloat16()
+    ws, stream = qc.qlinear_fp8_workspace_t(M, K, N), torch.cuda.current_stream().cuda_stream
+    ws.fill_(0xff)
+    assert qc.qc_qlinear_fp8_quant(X.data_ptr(), qc._xdt(X), M, K, ws.data_ptr(), ws.numel(), stream) == qc.QC_OK
+    for pw in (weights[0], weights[1], weights[0]):
+        bias = torch.randn(pw.N, generator=g, device="cuda")
+        Y = torch.full((M, pw.N), float("nan"), dtype=DTYPE[out], device="cuda")
+        assert qc.qc_qlinear_fp8_gemm(ws.data_ptr(), ws.numel(), M, K, pw.blob.data_ptr(), pw.scale.data_ptr(), pw.N, bias.data_ptr(),
+                                      qc.EPI["gelu_tanh"], Y.data_ptr(), qc.OUT[out], stream) == qc.QC_OK
+        assert torch.equal(Y, qc.qlinear_fp8_t(X, pw, bias, "gelu_tanh", out))
+
+
+@pytest.mark.parametrize("grouped", [False, True])
+@pytest.mark.parametrize("place", ["same", "behind", "before"])
+@pytest.mark.parametrize("what,K,N,outs", RING)
+def test_output_over_its_input_on_the_ring(what, K, N, outs, place, grouped):
+    """Y and X begin at the same address, or one some rows into the other: the bits of a call with both apart."""
+    out, E = ("bf16", "f32")[outs - 1], 3 if grouped else 0
+    M = rows_for(what, K, N, out, E)
+    assert which(M, K, N, out, E) == what
+    g = generator(K)
+    pw = random_weight(g, max(E, 1), N, K)
+    size, element = torch.finfo(DTYPE[out]).bits // 8, 2
+    far = 16 * K * element * 3 // 16 * 16
+    x_at, y_at = (far if place == "before" else 0), (far if place == "behind" else 0)
+    both = torch.empty(far + max(M * K * element, M * N * size), dtype=torch.uint8, device="cuda")
+    X = both[x_at:x_at + M * K * element].view(torch.bfloat16).view(M, K)
+    Y = both[y_at:y_at + M * N * size].view(DTYPE[out]).view(M, N)
+    apart = torch.randn(M, K, generator=g, device="cuda").bfloat16()
+    X.copy_(apart)
+    off = torch.tensor([0, M // 2 + 1, M // 2 + 1, M], dtype=torch.int32, device="cuda")
+    if grouped:
+        want = qc.qlinear_fp8_grouped_t(apart, pw, off, out=out)
+        qc.qlinear_fp8_grouped_t(X, pw, off, out=out, Y=Y)
+    else:
+        want = qc.qlinear_fp8_t(apart, pw, out=out)
+        qc.qlinear_fp8_t(X, pw, out=out, Y=Y)
+    assert torch.equal(Y, want)
+
+
+@pytest.mark.parametrize("grouped", [False, True])
+@pytest.mark.parametrize("what,K,N,outs", ONE_LAUNCH)
+def test_output_over_its_input_where_apart_it_is_one_launch(what, K, N, outs, grouped):
+    """Quantized in a launch of its own then, and the sums in another order: within what the order can change."""
+    E = 3 if grouped else 0
+    M = rows_for(what, K, N, "f32", E)
+    assert which(M, K, N, "f32", E) == what
+    g = generator(K + 1)
+    pw = random_weight(g, max(E, 1), N, K)
+    both = torch.empty(M * max(K, N), device="cuda")
+    X, Y = both[:M * K].view(M, K), both[:M * N].view(M, N)
+    X.copy_(torch.randn(M, K, generator=g, device="cuda"))
+    apart = X.clone()
+    off = torch.tensor([0, M // 2, M // 2, M], dtype=torch.int32, device="cuda")
+    call = (lambda *a, **k: qc.qlinear_fp8_grouped_t(*a[:2], off, **k)) if grouped else qc.qlinear_fp8_t
+    want = call(apart, pw, out="f32")
+    # sums of as many magnitudes: the linear of the dequantized operands' absolute values
+    q, s = qc.quant_act_fp8_t(apart)
+    kb = torch.arange(K, device="cuda") // 128
+    x = (q.double() * s.double()[:, kb]).abs()
+    codes, nb = qc.unpack_weight_codes_fp8_t(pw), torch.arange(N, device="cuda") // 128
+    magnitudes = torch.zeros(M, N, dtype=torch.float64, device="cuda")
+    for e, (lo, hi) in enumerate(zip(off.tolist(), off.tolist()[1:]) if grouped else [(0, M)]):
+        w = (codes[e].double() * pw.scale[e].double()[nb][:, kb]).abs()
+        magnitudes[lo:hi] = x[lo:hi] @ w.t().contiguous()
+    call(X, pw, out="f32", Y=Y)
+    # a block's products are added alike; of the blocks' sums either order rounds once a block, and each product with its scales twice
+    assert bool(((Y.double() - want.double()).abs() <= 2 * (-(-K // 128) + 3) * 2.0 ** -24 * magnitudes).all())
+
+
+def test_native_helpers_take_every_argument():
+    """Calls that succeed, in positions and by name, with a bias of each row: the Python helpers' bits."""
+    qc._use_native_helpers()
+    g = generator(8)
+    for M, N in ((40, 72), (700, 1304)):
+        K = 260
+        assert which(M, K, N, "bf16")[0] == which(M, K, N, "bf16", 3)[0] == ("few" if M == 40 else "ring")
+        X = torch.randn(M, K, generator=g, device="cuda")
+        pw, one = random_weight(g, 3, N, K), random_weight(g, 1, N, K)
+        off, bias = torch.tensor([0, 11, 11, M], dtype=torch.int32, device="cuda"), torch.randn(3, N, generator=g, device="cuda")
+        ws = qc.qlinear_fp8_workspace_t(M, K, N)
+        for epi in qc.EPI:
+            for out in ("bf16", "f32"):
+                for x in (X, X.bfloat16()):
+                    outputs = [torch.full((M, N), float("nan"), dtype=DTYPE[out], device="cuda") for _ in range(6)]
+                    plain = [f(x, one, bias[1], epi, out, ws, y) for f, y in zip((qc._python_helpers["qlinear_fp8_t"], qc.qlinear_fp8_t), outputs)]
+                    plain.append(qc.qlinear_fp8_t(x, one, workspace=ws, bias=bias[1], Y=outputs[2], epi=epi, out=out))
+                    grouped = [f(x, pw, off, bias, epi, out, ws, y)
+                               for f, y in zip((qc._python_helpers["qlinear_fp8_grouped_t"], qc.qlinear_fp8_grouped_t), outputs[3:])]
+                    grouped.append(qc.qlinear_fp8_grouped_t(x, pw, Y=outputs[5], out=out, expert_offsets=off, epi=epi, bias=bias, workspace=ws))
+                    assert all(a is b for a, b in zip(plain + grouped, outputs))
+                    assert all(torch.isfinite(t).all() and torch.equal(t, ts[0]) for ts in (plain, grouped) for t in ts), (M, epi, out, x.dtype)
