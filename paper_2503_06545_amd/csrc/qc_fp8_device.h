@@ -43,9 +43,9 @@ __device__ inline uint32_t e4m3x4(float q0, float q1, float q2, float q3) {
 }
 
 // One operand of 16 rows x 128 k as the matrix unit takes it.  The instructions for e4m3 operands line up eight products with
-// the largest of them before they add, and drop what is then too low: the sum of a block comes out 1.5e-5 off (2-norm,
-// normal values), where the instruction for bf16 operands is 1e-8 off.  That is enough for outputs that are rounded to bf16
-// (2^-9 each), not for binary32 ones.  EXACT widens the codes to bf16, exactly, and takes four instructions of 32 k instead
+// the largest of them before they add, and cut off what is then too low: the sum of a block comes out 1.4e-5 off (2-norm,
+// normal values; 2.2e-5 after GELU, 8e-5 and towards zero for positive values spread over twelve powers of two), where the
+// instruction for bf16 operands is 1e-8 off.  That is enough for outputs that are rounded to bf16 (by up to 2^-8 of each), not for binary32 ones.  EXACT widens the codes to bf16, exactly, and takes four instructions of 32 k instead
 // of one of 128 (registers only, random operands, TFLOP/s: 4390 and 2260).
 template <bool EXACT>
 struct Operand;

@@ -274,3 +274,87 @@ def test_native_helpers_take_every_argument():
                     grouped.append(qc.qlinear_fp8_grouped_t(x, pw, Y=outputs[5], out=out, expert_offsets=off, epi=epi, bias=bias, workspace=ws))
                     assert all(a is b for a, b in zip(plain + grouped, outputs))
                     assert all(torch.isfinite(t).all() and torch.equal(t, ts[0]) for ts in (plain, grouped) for t in ts), (M, epi, out, x.dtype)
+
+
+# ---- how exact -----------------------------------------------------------------------------------
+
+def whole_numbers(g, rows, K, groups, other):
+    """[rows, K] of whole numbers up to 15 times a power of two for each run of 128 columns of a row, or, with `groups`, of 128 rows,
+    whose largest magnitude is 448 of them, so that the scales are these powers and the codes the numbers.  The column that holds
+    the 448 meets a zero of the other operand; where a run is too short for such columns every value is one."""
+    steps = torch.randint(0, 2, (-(-rows // 128) if groups else rows, -(-K // 128)), generator=g, device="cuda")
+    v = torch.randint(-15, 16, (rows, K), generator=g, device="cuda").float()
+    for b in range(-(-K // 128)):
+        at, width = 128 * b, min(128, K - 128 * b)
+        if width < 3:
+            v[:, at:at + width] = 448.0 * torch.sign(v[:, at:at + width] + 0.5)
+        else:
+            v[:, at + (5 * b + other) % width], v[:, at + (5 * b + 1 - other) % width] = 448.0, 0.0
+    steps = steps.repeat_interleave(128, dim=0)[:rows] if groups else steps
+    return v * 2.0 ** steps.repeat_interleave(128, dim=1)[:, :K]
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("grouped", [False, True])
+@pytest.mark.parametrize("what,K,N,out", EVERY)
+def test_whole_numbers_come_out_exactly(what, K, N, out, grouped, x):
+    """Every product is a whole number of magnitude 225 at most, seven powers of two above 1, which the e4m3 instruction keeps, or 448 * 448 alone with
+    its like, and every sum below 2^24: nothing is rounded before the output.  Each token and each 128 x 128 has scales of its own."""
+    E = 3 if grouped else 1
+    M = rows_for(what, K, N, out, E if grouped else 0)
+    assert which(M, K, N, out, E if grouped else 0) == what
+    g = generator(M + N + K)
+    X = whole_numbers(g, M, K, False, 0)
+    W = torch.stack([whole_numbers(g, N, K, True, 1) for _ in range(E)])
+    bias = torch.randint(-100, 101, (E, N), generator=g, device="cuda").float()
+    pw = qc.pack_weight_fp8_t(W if grouped else W[0])
+    assert bool((torch.log2(pw.scale) == torch.log2(pw.scale).round()).all())
+    cut = [1, 1 + M // 2, 1 + M // 2, M - 1] if grouped else [0, M]
+    want = torch.full((M, N), 9.0, dtype=torch.float64, device="cuda")
+    for e, (lo, hi) in enumerate(zip(cut, cut[1:])):
+        want[lo:hi] = X[lo:hi].double() @ W[e].double().t().contiguous() + bias[e].double()
+    assert want.abs().max() < 2 ** 24
+    Y = torch.full((M, N), 9.0, dtype=DTYPE[out], device="cuda")
+    if grouped:
+        qc.qlinear_fp8_grouped_t(X.to(DTYPE[x]), pw, torch.tensor(cut, dtype=torch.int32, device="cuda"), bias, out=out, Y=Y)
+    else:
+        qc.qlinear_fp8_t(X.to(DTYPE[x]), pw, bias[0], out=out, Y=Y)
+    assert torch.equal(Y, want.to(DTYPE[out]))
+
+
+def errors_before_rounding(g, what, K, N, values):
+    """(errors, sums, sums of magnitudes) of the outputs of one token, all in 64 bits: its bias takes the sums away, so that
+    what is left is rounded relative to itself.  All rows are that token."""
+    M = rows_for(what, K, N, "bf16")
+    assert which(M, K, N, "bf16") == what
+    x, W = values(g, 1, K).bfloat16(), values(g, N, K)
+    pw = qc.pack_weight_fp8_t(W)
+    q, s = qc.quant_act_fp8_t(x)
+    kb, nb = torch.arange(K, device="cuda") // 128, torch.arange(N, device="cuda") // 128
+    xd = q.double() * s.double()[:, kb]
+    wd = qc.unpack_weight_codes_fp8_t(pw)[0].double() * pw.scale[0].double()[nb][:, kb]
+    sums, magnitudes = (xd * wd).sum(dim=1), (xd * wd).abs().sum(dim=1)
+    bias = -sums.float()
+    y = qc.qlinear_fp8_t(x.expand(M, K).contiguous(), pw, bias)
+    assert bool((y == y[0]).all())
+    return y[0].double() - (sums + bias.double()), sums, magnitudes
+
+
+def normal(g, rows, K):
+    return torch.randn(rows, K, generator=g, device="cuda")
+
+
+def spread(g, rows, K):   # over twelve powers of two
+    return torch.exp2(-12.0 * torch.rand(rows, K, generator=g, device="cuda"))
+
+
+@pytest.mark.parametrize("what,K,N", [k[:3] for k in KERNELS])
+def test_how_far_off_bf16_outputs_are_before_they_are_rounded(what, K, N):
+    """The figures that the interface names, 1.4e-5 of normal values' sums and 8e-5 of those of values spread over twelve powers of two (2-norms over
+    many channels, one token: their spread is a tenth or so), with a factor of two; and for each output what a group of eight can lose."""
+    g = generator(K)
+    for values, figure in ((normal, 1.4e-5), (spread, 8e-5)):
+        error, sums, magnitudes = errors_before_rounding(g, what, K, N, values)
+        assert error.norm() <= 2 * figure * sums.norm(), (values.__name__, float(error.norm() / sums.norm()))
+        # beside it the sums in binary32 and the rounding of what is left
+        assert bool((error.abs() <= (7 * 2.0 ** -13 + (-(-K // 128) + 3) * 2.0 ** -24) * (1 + 2.0 ** -8) * magnitudes).all()), values.__name__
