@@ -8,6 +8,9 @@
 
 #include "qc_fp8_device.h"
 
+// The copies to LDS name m0, which they set, among what they clobber; the compiler, which keeps it for itself, warns of that.
+#pragma clang diagnostic ignored "-Winline-asm"
+
 namespace qc {
 namespace {
 
@@ -101,11 +104,11 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_ring_kernel(Fp8GemmArgs a) {
         asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:%4\n\t" \
                      "global_load_lds_dwordx4 %1, %2 offset:%5\n\tglobal_load_lds_dwordx4 %1, %2 offset:%6"    \
                      ::"s"(lds_w), "v"(lane16), "s"(wnext), "n"((slot) * kFp8TileBytes), "n"(kFragBytes), "n"(2 * kFragBytes), \
-                     "n"(3 * kFragBytes) : "memory", "scc");                                                   \
+                     "n"(3 * kFragBytes) : "memory", "scc", "m0");                                                 \
         wnext += kFp8TileBytes;                                                                                \
     } while (0)
 #define QC_COPY_4(at_lds, imm, off, base) \
-    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(at_lds), "v"(off), "s"(base), "n"(imm) : "memory", "scc")
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(at_lds), "v"(off), "s"(base), "n"(imm) : "memory", "scc", "m0")
     // the channel tile's scales and biases, without a wait of their own: ahead of the first weights
     for (int b = wave * 64; b < KB; b += kThreads)
         QC_COPY_4((uint32_t)(uintptr_t)(lds_sw + b), 0, 4u * min(b + lane, KB - 1), a.w_scale + ((int64_t)at.expert * a.n_tiles + nt) * KB);
