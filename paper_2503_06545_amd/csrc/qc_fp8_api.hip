@@ -66,7 +66,10 @@ Fp8GemmArgs gemm_args(void *workspace, int64_t M, int64_t K, const void *packed,
     a.KB = (int)ws.KB;
     a.m_tiles = (int)(grouped ? fp8_tiles_most(M, experts, plan.tokens) : (M + plan.tokens - 1) / plan.tokens);
     a.n_tiles = (int)(round_up(N, kTileN) / kTileN);
-    a.group_m = a.n_tiles > 16 ? 8 : (a.KB >= 18 ? 3 : 2);
+    // Token tiles of the patch that the blocks of an XCD work on: eight where there are many channel tiles, else three, as good as
+    // two and four there (us at 3 and 8: 131072 x 1152 x 4608 691 678, 32768 x 1152 x 4608 of 16 experts 211 208; 65536 x 4608 x 1152 308 311,
+    // of 64 experts 524 566, 12000 x 9216 x 1152 118 121, 40000 x 640 x 1800 65.6 67.1).
+    a.group_m = a.n_tiles > 16 ? 8 : 3;
     return a;
 }
 
