@@ -276,9 +276,10 @@ qc_status qc_qlinear_tensor(const void *X, qc_dtype xdt, int64_t M, int64_t K, i
  * With QC_OUT_BF16 the products of a block go through the matrix unit's e4m3 form, which cuts off what is more than 13 powers
  * of two below the largest of every eight products; the blocks are added in binary32.  Sums of normal values come out 1.4e-5 off by it
  * (2-norm), sums of values spread over twelve powers of two 8e-5, always towards zero where their signs are one, and never more than
- * 7 * 2^-13 of the magnitudes that go in; the rounding to bf16 is off by up to 2^-8 of the output.  The order depends
- * on the sizes of the call, so the same token may differ in the last bits between calls of other sizes, never between
- * calls of the same.  A NaN or an infinity in X makes its token's outputs NaN and touches no other token's.
+ * 7 * 2^-13 of the magnitudes that go in; the rounding to bf16 is off by up to 2^-8 of the output.  The order of the
+ * blocks' sums depends on M, K, N, the number of experts, the types of X and Y, whether Y lies over X, and whether a call is made whole
+ * or in halves: the same token may differ in the last bits between calls that differ in one of these, never between calls
+ * that agree in them.  A NaN or an infinity in X makes its token's outputs NaN and touches no other token's.
  *   qc_pack_weight_fp8    W: device, float [experts, N, K] (experts = 1: one linear's matrix).  packed: device,
  *                         qc_packed_weight_fp8_bytes(experts, N, K) bytes, 256-byte aligned, opaque.  w_scale:
  *                         device, float [experts, ceil(N / 128), ceil(K / 128)]

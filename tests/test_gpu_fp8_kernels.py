@@ -276,6 +276,30 @@ def test_native_helpers_take_every_argument():
                     assert all(torch.isfinite(t).all() and torch.equal(t, ts[0]) for ts in (plain, grouped) for t in ts), (M, epi, out, x.dtype)
 
 
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("what,K,N,out", EVERY)
+def test_calls_that_agree_in_all_but_addresses_give_the_same_bits(what, K, N, out, x):
+    """Other buffers, another workspace that held something else, and another stream."""
+    M, E = rows_for(what, K, N, out), 3
+    G = rows_for(what, K, N, out, E)
+    assert which(M, K, N, out) == which(G, K, N, out, E) == what
+    g = generator(M + 2)
+    one, pw = random_weight(g, 1, N, K), random_weight(g, E, N, K)
+    X = torch.randn(max(M, G), K, generator=g, device="cuda").to(DTYPE[x])
+    off = torch.tensor([0, G // 3, G // 2, G], dtype=torch.int32, device="cuda")
+    want = qc.qlinear_fp8_t(X[:M], one, out=out), qc.qlinear_fp8_grouped_t(X[:G], pw, off, out=out)
+    other, again = torch.cuda.Stream(), X.clone()
+    ws = qc.qlinear_fp8_workspace_t(max(M, G), K, N)
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        got = []
+        for fill in (0x00, 0xff):
+            ws.fill_(fill)
+            got += [qc.qlinear_fp8_t(again[:M], one, out=out, workspace=ws), qc.qlinear_fp8_grouped_t(again[:G], pw, off, out=out, workspace=ws)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[i % 2]) for i, y in enumerate(got))
+
+
 # ---- how exact -----------------------------------------------------------------------------------
 
 def whole_numbers(g, rows, K, groups, other):
