@@ -346,6 +346,20 @@ def test_whole_numbers_come_out_exactly(what, K, N, out, grouped, x):
     assert torch.equal(Y, want.to(DTYPE[out]))
 
 
+@pytest.mark.parametrize("what,K,N,out", EVERY)
+def test_scales_far_from_one(what, K, N, out):
+    """Powers of two on either operand come out as their product, as long as the scales' product is a normal number.  (A product of
+    codes is below 2^18, a sum of them below 2^24: with the largest powers here outputs stay below 2^124.)"""
+    M = rows_for(what, K, N, out)
+    assert which(M, K, N, out) == what
+    g = generator(M * 2 + K)
+    X, W = whole_numbers(g, M, K, False, 0), whole_numbers(g, N, K, True, 1)
+    want = X.double() @ W.double().t().contiguous()
+    for a, b in ((-50, -60), (-60, -65), (50, 50), (60, -60), (-60, 60), (90, 8), (-60, 100)):
+        y = qc.qlinear_fp8_t(X * 2.0 ** a, qc.pack_weight_fp8_t(W * 2.0 ** b), out=out)
+        assert torch.equal(y, (want * 2.0 ** (a + b)).to(DTYPE[out])), (a, b)
+
+
 def errors_before_rounding(g, what, K, N, values):
     """(errors, sums, sums of magnitudes) of the outputs of one token, all in 64 bits: its bias takes the sums away, so that
     what is left is rounded relative to itself.  All rows are that token."""
