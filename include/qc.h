@@ -284,9 +284,12 @@ qc_status qc_qlinear_tensor(const void *X, qc_dtype xdt, int64_t M, int64_t K, i
  * that agree in them.  A NaN or an infinity in X makes its token's outputs NaN and touches no other token's.
  *   qc_pack_weight_fp8    W: device, float [experts, N, K] (experts = 1: one linear's matrix).  packed: device,
  *                         qc_packed_weight_fp8_bytes(experts, N, K) bytes, 256-byte aligned, opaque.  w_scale:
- *                         device, float [experts, ceil(N / 128), ceil(K / 128)]
+ *                         device, float [experts, ceil(N / 128), ceil(K / 128)].  Codes and scales of a checkpoint are
+ *                         widened to float first; quantized again they are the same codes, and scales to an ulp, in blocks
+ *                         whose largest code is 448, others are rounded once more
  *   qc_unpack_weight_codes_fp8   test hook: the codes of a packed blob, uint8 [experts, N, K]
- *   qc_quant_act_fp8      qx: device, uint8 [M, K]; x_scale: device, float [M, ceil(K / 128)]
+ *   qc_quant_act_fp8      qx: device, uint8 [M, K]; x_scale: device, float [M, ceil(K / 128)]: for other readers of the codes, the
+ *                         linears below take X and keep codes in an order of their own
  *   qc_qlinear_fp8        quantize + GEMM + epilogue.  workspace >= qc_qlinear_fp8_workspace_bytes(M, K, N) bytes,
  *                         256-byte aligned, contents irrelevant on entry and unspecified on exit.  Y: QC_OUT_F32 or
  *                         QC_OUT_BF16; may lie over X as for qc_qlinear
