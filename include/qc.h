@@ -290,8 +290,8 @@ qc_status qc_qlinear_tensor(const void *X, qc_dtype xdt, int64_t M, int64_t K, i
  *   qc_unpack_weight_codes_fp8   test hook: the codes of a packed blob, uint8 [experts, N, K]
  *   qc_quant_act_fp8      qx: device, uint8 [M, K]; x_scale: device, float [M, ceil(K / 128)]: for other readers of the codes, the
  *                         linears below take X and keep codes in an order of their own
- *   qc_qlinear_fp8        quantize + GEMM + epilogue.  workspace >= qc_qlinear_fp8_workspace_bytes(M, K, N) bytes,
- *                         256-byte aligned, contents irrelevant on entry and unspecified on exit.  Y: QC_OUT_F32 or
+ *   qc_qlinear_fp8        quantize + GEMM + epilogue.  workspace >= qc_qlinear_fp8_workspace_bytes(M, K, N) bytes
+ *                         (0: a size that is refused), 256-byte aligned, contents irrelevant on entry and unspecified on exit.  Y: QC_OUT_F32 or
  *                         QC_OUT_BF16; may lie over X as for qc_qlinear
  *   qc_qlinear_fp8_quant, qc_qlinear_fp8_gemm   two halves as calls of their own, for one input of several linears: the
  *                         first leaves codes and scales in the workspace, the second may run on them repeatedly.  Their result
@@ -305,7 +305,7 @@ qc_status qc_qlinear_tensor(const void *X, qc_dtype xdt, int64_t M, int64_t K, i
  *                         unspecified, but nothing outside X, Y and the workspace is touched.  Same
  *                         workspace as qc_qlinear_fp8
  * Errors as for qc_qlinear; UNSUPPORTED also: QC_OUT_I32_ACC, experts > QC_MAX_EXPERTS, M >= 2^31, and sizes for which a launch
- * would need more than 2^24 blocks. */
+ * would need 2^24 - 1 blocks of 256 threads or more (a block quantizes 32 tokens x 128 columns, or multiplies a tile). */
 #define QC_FP8_BLOCK 128
 size_t qc_packed_weight_fp8_bytes(int64_t experts, int64_t N, int64_t K);
 qc_status qc_pack_weight_fp8(const float *W, int64_t experts, int64_t N, int64_t K, void *packed, float *w_scale,

@@ -123,7 +123,7 @@ extern "C" qc_status qc_quant_act_fp8(const void *X, qc_dtype xdt, int64_t M, in
 }
 
 extern "C" size_t qc_qlinear_fp8_workspace_bytes(int64_t M, int64_t K, int64_t N) {
-    if (M < 1 || K < 1 || N < 1 || K > QC_MAX_K) return 0;
+    if (M < 1 || K < 1 || N < 1 || N > QC_MAX_N || check_quant_supported(M, K) != QC_OK) return 0;
     return fp8_workspace(M, K).total_bytes;
 }
 
