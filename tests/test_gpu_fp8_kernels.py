@@ -360,6 +360,36 @@ def test_scales_far_from_one(what, K, N, out):
         assert torch.equal(y, (want * 2.0 ** (a + b)).to(DTYPE[out])), (a, b)
 
 
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N,experts", [(3, 100, 2200001, 0), (5, 260, 1100000, 2)])
+def test_millions_of_channels(M, K, N, experts, out):
+    """More than the rule for few tokens counts, one tile of tokens high."""
+    assert which(M, K, N, out, experts)[0] == "ring"
+    g = generator(N)
+    X = whole_numbers(g, M, K, False, 0)
+    W = torch.stack([whole_numbers(g, N, K, True, 1) for _ in range(max(experts, 1))])
+    cut = [0, 2, M] if experts else [0, M]
+    want = torch.cat([X[lo:hi].double() @ W[e].double().t() for e, (lo, hi) in enumerate(zip(cut, cut[1:]))])
+    pw = qc.pack_weight_fp8_t(W if experts else W[0])
+    if experts:
+        y = qc.qlinear_fp8_grouped_t(X, pw, torch.tensor(cut, dtype=torch.int32, device="cuda"), out=out)
+    else:
+        y = qc.qlinear_fp8_t(X, pw, out=out)
+    assert torch.equal(y, want.to(DTYPE[out]))
+
+
+def test_weights_beyond_four_gib():
+    """The last channels' codes lie past 2^32 bytes; the rows of a few tiles of channels repeated, against those alone."""
+    M, K, period, N = 3, 2000, 7 * 128, 2200001
+    assert which(M, K, N, "bf16")[0] == "ring" and qc.qc_packed_weight_fp8_bytes(1, N, K) > 2 ** 32
+    g = generator(K)
+    X, W = whole_numbers(g, M, K, False, 0), whole_numbers(g, period, K, True, 1)
+    want = (X.double() @ W.double().t()).bfloat16()
+    y = qc.qlinear_fp8_t(X, qc.pack_weight_fp8_t(W.repeat(-(-N // period), 1)[:N]))
+    whole = N // period * period
+    assert bool((y[:, :whole].reshape(M, -1, period) == want[:, None]).all()) and torch.equal(y[:, whole:], want[:, :N - whole])
+
+
 def errors_before_rounding(g, what, K, N, values):
     """(errors, sums, sums of magnitudes) of the outputs of one token, all in 64 bits: its bias takes the sums away, so that
     what is left is rounded relative to itself.  All rows are that token."""
